@@ -65,8 +65,9 @@ typedef enum {
 } srs_error;
 
 /* device flags reported by srs_status() */
-#define SRS_FLAG_OVERFLOW  1u  /* extract: some bucket had more than cap changed elements */
-#define SRS_FLAG_BAD_INDEX 2u  /* apply: an index lay outside its bucket's span and was skipped */
+#define SRS_FLAG_OVERFLOW  1u  /* extract: some bucket had more than cap changed elements; cache tables: pages, table or rows ran out */
+#define SRS_FLAG_BAD_INDEX 2u  /* apply: an index lay outside its bucket's span and was skipped; cache calls: a length, slot or page was
+                                  outside its range */
 #define SRS_FLAG_TIMEOUT   4u  /* extract: a tile gave up waiting for its predecessors, or the scratch was found out of order
                                   because calls that share it had overlapped (payload invalid) */
 
@@ -351,6 +352,110 @@ int srs_pack_dense_multi(srs_ctx *ctx, srs_plan *plan, const srs_tensor_pair *t,
                          const uint32_t *n_dense, uint32_t max_dense, uint16_t *dense, void *stream);
 int srs_unpack_dense_multi(srs_ctx *ctx, srs_plan *plan, const srs_tensor *t, const int32_t *dense_bucket,
                            const uint32_t *n_dense, uint32_t max_dense, const uint16_t *dense, void *stream);
+
+/*
+ * The Rollout's key/value cache.  A synchronisation leaves the keys and values that running requests have cached as the old weights
+ * made them: they are computed again with the new ones, or the cache is kept and grows by single tokens.  These calls are the cache's
+ * side of either.  The cache is paged: `pages` pages of `page_tokens` tokens, and a request's tokens lie in the pages that its row of
+ * the block table names, token j in place j % page_tokens of page table[r*table_width + j / page_tokens].  A slot is a place in the
+ * cache, page * page_tokens + place.  Everything that varies from step to step (lengths, tables, slots, what is left of the free
+ * pages) is device memory, so that steps can be queued, or replayed from a graph, without the host waiting for any of it.
+ */
+
+/*
+ * Block tables, slots and positions of the new tokens of nrequests requests.  Request r has start[r] tokens that stay as they are,
+ * count[r] new ones behind them (0 is allowed) and holds held[r] pages: the first held[r] entries of its row of table[nrequests *
+ * table_width].  Where start[r] + count[r] tokens need more pages it gets them from the free list free_pages[0 .. *free_count), from
+ * its end, requests in ascending order; their numbers are entered in its row, held[r] and *free_count are updated.  A request whose
+ * tokens were all made with old weights is re-encoded with start[r] = 0 and count[r] its length: it keeps its pages and takes none.
+ *   token_begin[nrequests + 1]  number of new tokens before request r: its rows in the step's batch
+ *   slots[max_tokens], positions[max_tokens]  of every row: where its key and value go, and its position in the request.  Rows behind
+ *                               the last request's (a batch padded to a fixed size) have slot -1 and position 0.
+ * Where the free pages do not suffice the first ones to ask get them, the others' tokens have slot -1, as have tokens beyond table_width
+ * pages; rows beyond max_tokens are left out and token_begin stops at max_tokens; each raises SRS_FLAG_OVERFLOW.  A negative start, count
+ * or held, a held beyond table_width and a *free_count outside 0 .. free_cap are taken as the nearest value allowed and raise
+ * SRS_FLAG_BAD_INDEX.  table_width * page_tokens and max_tokens must be below 2^31; max_tokens = 0 takes NULL slots and positions.
+ *
+ * srs_cache_release gives pages back: request r keeps its first keep[r] pages (0: none; at least held[r]: all), the others go to the
+ * end of the free list in the reverse of the order in which one call of srs_cache_tables hands them out, so that it undoes that call.
+ * Table entries are left as they are.  Pages that would not fit the list (more than free_cap in all) are dropped and raise SRS_FLAG_OVERFLOW.
+ */
+int srs_cache_tables(srs_ctx *ctx, const int32_t *start, const int32_t *count, uint32_t nrequests, uint32_t page_tokens,
+                     int32_t *held, int32_t *table, uint32_t table_width, const int32_t *free_pages, int32_t *free_count,
+                     uint32_t free_cap, int32_t *token_begin, int64_t *slots, int32_t *positions, uint64_t max_tokens, void *stream);
+int srs_cache_release(srs_ctx *ctx, const int32_t *keep, uint32_t nrequests, int32_t *held, const int32_t *table,
+                      uint32_t table_width, int32_t *free_pages, int32_t *free_count, uint32_t free_cap, void *stream);
+
+/* Element types of the calls below. */
+#define SRS_BF16 0
+#define SRS_FP16 1
+#define SRS_FP32 2
+
+/* Rows of heads, one per token: element d of head h of token t is p[t*token_stride + h*head_stride + d] (strides in elements). */
+typedef struct {
+    void *p;
+    uint32_t heads;
+    int64_t token_stride, head_stride;
+} srs_rows;
+
+/* A paged cache: element d of key head h in place s of page g is k[g*k_page + s*k_token + h*k_head + d] (strides in elements). */
+typedef struct {
+    void *k, *v;
+    int dtype;
+    uint32_t pages, page_tokens, heads, head_dim;
+    int64_t k_page, k_token, k_head, v_page, v_token, v_head;
+} srs_cache;
+
+/*
+ * Rotary positions.  The first rot_dim elements of every head (even, at most head_dim) are turned in pairs, the others copied: with
+ * pair i = (x[i], x[i + rot_dim/2]), or (x[2i], x[2i+1]) with SRS_ROPE_INTERLEAVED, and a = positions[t] * inv_freq[i],
+ *     out = magnitude * (x1 cos a - x2 sin a, x2 cos a + x1 sin a).
+ * SRS_ROPE_TRANSPOSE turns by -a: with the same magnitude it takes the gradient of out to that of x.  inv_freq[rot_dim / 2] and the
+ * magnitude carry whatever scaling for long contexts the model has.  The angle is taken in double, as far positions need; sine,
+ * cosine and the products are binary32, rounded once to the element type (nearest, ties to even).
+ * Any strides, alignment and head sizes; out may be x with the same strides, and otherwise overlaps nothing.
+ */
+#define SRS_ROPE_INTERLEAVED 1u
+#define SRS_ROPE_TRANSPOSE   2u
+int srs_rope(srs_ctx *ctx, int dtype, const srs_rows *x, const srs_rows *out, uint64_t tokens, uint32_t head_dim,
+             const int32_t *positions, const double *inv_freq, uint32_t rot_dim, uint32_t flags, float magnitude, void *stream);
+
+/*
+ * New keys and values into the cache: row t of k and v (cache->heads heads each) goes to slot slots[t]; -1 is left out, another slot
+ * outside the cache is left out and raises SRS_FLAG_BAD_INDEX, a slot that comes twice is a caller error (one of the rows wins).  With
+ * rot_dim > 0 keys are turned as in srs_rope on the way (positions, inv_freq, flags, magnitude as there), and where q is given q_out
+ * receives the turned queries of every row, whatever its slot; with rot_dim = 0 positions, inv_freq, q and q_out are not used.
+ * q_out may be q with the same strides.  Any strides and alignment.
+ */
+int srs_cache_write(srs_ctx *ctx, const srs_cache *cache, const srs_rows *k, const srs_rows *v, uint64_t tokens,
+                    const int64_t *slots, const srs_rows *q, const srs_rows *q_out, const int32_t *positions, const double *inv_freq,
+                    uint32_t rot_dim, uint32_t flags, float magnitude, void *stream);
+
+/*
+ * Attention of new tokens over the paged cache.  Request r has the rows token_begin[r] .. token_begin[r+1] of q and out, and its keys
+ * are the first start[r] + count tokens of its row of table (count = its number of rows; the new tokens' own keys are in the cache
+ * already).  The row at position p = start[r] + i sees the keys j <= p, with window > 0 of them those with p - j < window or j < sinks:
+ *     s_j = scale * q . k_j,   out = sum_j exp(s_j) v_j / sum_j exp(s_j),   lse = log sum_j exp(s_j)
+ * Query head h reads key head h / (q->heads / cache->heads).  With SRS_ATTN_FULL every row sees all start[r] + count keys (window and sinks 0).  A row that sees no key is 0, its lse -inf.  Hidden keys and values do not enter,
+ * whatever their bits are.  Rows outside every request are left as they are.  Sums, maxima and products are binary32; the weights
+ * exp(s_j) are rounded to the element type before they meet the values unless a kernel carries them in two parts; out is rounded once.
+ * q, out and cache are BF16 or FP16; head_dim a multiple of 8 up to 256; q->heads a multiple of cache->heads; every pointer 16-byte
+ * aligned and every stride a multiple of 8 elements.  lse (tokens x q->heads, contiguous) may be NULL.  A page outside the cache that a
+ * row would read counts as hidden and raises SRS_FLAG_BAD_INDEX, as does a request whose rows lie outside 0 .. tokens (it is left out).  Keys
+ * beyond table_width pages are hidden and raise it too.
+ * most_tokens and most_keys: the largest count and the largest number of keys of a request, as far as the caller knows (0: unknown).
+ * They choose how the work is split, nothing else.
+ * workspace: device memory, 16-byte aligned, of at least srs_cache_attention_workspace bytes for the same sizes (0 bytes: none is needed);
+ * written and read by this call only, so calls that cannot overlap may share one.
+ */
+#define SRS_ATTN_FULL 1u
+uint64_t srs_cache_attention_workspace(uint32_t nrequests, uint64_t tokens, uint32_t q_heads, uint32_t kv_heads, uint32_t head_dim,
+                                       uint32_t table_width, uint32_t page_tokens, uint32_t window, uint32_t sinks,
+                                       uint64_t most_tokens, uint64_t most_keys);
+int srs_cache_attention(srs_ctx *ctx, const srs_cache *cache, const srs_rows *q, const srs_rows *out, float *lse, uint64_t tokens,
+                        const int32_t *token_begin, const int32_t *start, const int32_t *table, uint32_t table_width,
+                        uint32_t nrequests, float scale, uint32_t flags, uint32_t window, uint32_t sinks, uint64_t most_tokens,
+                        uint64_t most_keys, void *workspace, uint64_t workspace_bytes, void *stream);
 
 /*
  * Measurement aid (not part of the method): reads `bytes` bytes from each of a and b with the same

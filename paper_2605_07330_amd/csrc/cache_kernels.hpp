@@ -1,0 +1,262 @@
+// Device code of the cache calls for gfx950: block tables and slots from request lengths, rotary positions, rows into the paged cache.
+#pragma once
+#include "srs_kernels.hpp"
+
+namespace srs {
+
+// ---- block tables -----------------------------------------------------------------------------------------------------
+
+constexpr int kTableThreads = 1024;
+
+struct TablesArgs {
+    const int32_t *start, *count;
+    uint32_t nrequests, page;
+    int32_t *held, *table;
+    uint32_t width;
+    const int32_t *free_pages;
+    int32_t *free_count;
+    uint32_t free_cap;
+    int32_t *token_begin;
+    int64_t *slots;
+    int32_t *positions;
+    uint32_t max_tokens;
+    uint32_t *flags;
+};
+
+// Exclusive sums of two numbers per thread over the workgroup; totals in the last two.
+__device__ __forceinline__ void block_sums(int64_t a, int64_t b, int64_t &before_a, int64_t &before_b, int64_t &all_a, int64_t &all_b) {
+    __shared__ int64_t wave_sums[2][kTableThreads / 64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int64_t x = a, y = b;
+#pragma unroll
+    for (int k = 1; k < 64; k *= 2) {
+        const int64_t u = __shfl_up(x, k), v = __shfl_up(y, k);
+        if (lane >= k) { x += u; y += v; }
+    }
+    if (lane == 63) { wave_sums[0][wave] = x; wave_sums[1][wave] = y; }
+    __syncthreads();
+    all_a = all_b = 0;
+    before_a = x - a; before_b = y - b;
+#pragma unroll
+    for (int w = 0; w < kTableThreads / 64; ++w) {
+        if (w == wave) { before_a += all_a; before_b += all_b; }
+        all_a += wave_sums[0][w]; all_b += wave_sums[1][w];
+    }
+    __syncthreads();
+}
+
+// largest q < n with at[q] <= k (at ascending, at[0] <= k)
+__device__ __forceinline__ uint32_t last_at_most(const uint32_t *at, uint32_t n, uint32_t k) {
+    uint32_t lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const uint32_t mid = (lo + hi) / 2;
+        if (at[mid] <= k) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+// One workgroup.  Requests come in chunks of one per thread; their tokens and the pages they ask for are numbered by two prefix sums,
+// and both are then spread over all threads, which find their request by bisection.
+__global__ __launch_bounds__(kTableThreads) void cache_tables_kernel(const TablesArgs a) {
+    __shared__ uint32_t s_tok[kTableThreads + 1], s_page[kTableThreads + 1], s_start[kTableThreads], s_held[kTableThreads];
+    const uint32_t tid = threadIdx.x;
+    const int32_t listed = *a.free_count;
+    const uint32_t avail = listed < 0 ? 0u : (uint32_t)listed > a.free_cap ? a.free_cap : (uint32_t)listed;
+    uint32_t flags = (listed < 0 || (uint32_t)listed > a.free_cap) ? kFlagBadIndex : 0u;
+    int64_t tokens = 0, pages = 0;                          // of the requests before this chunk
+    for (uint32_t base = 0; base < a.nrequests; base += kTableThreads) {
+        const uint32_t r = base + tid, n = a.nrequests - base < (uint32_t)kTableThreads ? a.nrequests - base : (uint32_t)kTableThreads;
+        int64_t cnt = 0, want = 0;
+        uint32_t start = 0, held = 0;
+        if (tid < n) {
+            const int32_t s = a.start[r], c = a.count[r], h = a.held[r];
+            if (s < 0 || c < 0 || h < 0 || (uint32_t)(h < 0 ? 0 : h) > a.width) flags |= kFlagBadIndex;
+            start = s < 0 ? 0u : (uint32_t)s; cnt = c < 0 ? 0 : c; held = h < 0 ? 0u : (uint32_t)h > a.width ? a.width : (uint32_t)h;
+            const uint32_t need = (uint32_t)(((uint64_t)start + (uint64_t)cnt + a.page - 1) / a.page);
+            if (need > a.width && cnt > 0) flags |= kFlagOverflow;
+            const uint32_t most = need < a.width ? need : a.width;
+            want = most > held ? (int64_t)(most - held) : 0;
+        }
+        int64_t t0, p0, t_all, p_all;
+        block_sums(cnt, want, t0, p0, t_all, p_all);
+        t0 += tokens; p0 += pages;
+        const uint32_t tb = t0 < (int64_t)a.max_tokens ? (uint32_t)t0 : a.max_tokens, pb = p0 < (int64_t)avail ? (uint32_t)p0 : avail;
+        s_tok[tid] = tb; s_page[tid] = pb; s_start[tid] = start; s_held[tid] = held;
+        if (tid < n) a.token_begin[r] = (int32_t)tb;
+        tokens += t_all; pages += p_all;
+        const uint32_t t_end = tokens < (int64_t)a.max_tokens ? (uint32_t)tokens : a.max_tokens;
+        const uint32_t p_end = pages < (int64_t)avail ? (uint32_t)pages : avail;
+        if (tid == n - 1) { s_tok[n] = t_end; s_page[n] = p_end; }
+        __syncthreads();
+        if (tid < n && s_page[tid + 1] > pb) a.held[r] = (int32_t)(held + (s_page[tid + 1] - pb));
+        for (uint32_t k = s_page[0] + tid; k < p_end; k += kTableThreads) {
+            const uint32_t q = last_at_most(s_page, n, k);
+            a.table[(uint64_t)(base + q) * a.width + s_held[q] + (k - s_page[q])] = a.free_pages[avail - 1 - k];
+        }
+        for (uint32_t t = s_tok[0] + tid; t < t_end; t += kTableThreads) {
+            const uint32_t q = last_at_most(s_tok, n, t);
+            const uint32_t pos = s_start[q] + (t - s_tok[q]), at = pos / a.page, h = s_held[q], got = s_page[q + 1] - s_page[q];
+            int32_t page = -1;
+            if (at < h) page = a.table[(uint64_t)(base + q) * a.width + at];
+            else if (at - h < got) page = a.free_pages[avail - 1 - (s_page[q] + (at - h))];
+            a.slots[t] = page < 0 ? -1ll : (int64_t)page * a.page + (pos - at * a.page);
+            a.positions[t] = pos > 0x7fffffffu ? 0x7fffffff : (int32_t)pos;
+        }
+        __syncthreads();
+    }
+    if (tokens > (int64_t)a.max_tokens || pages > (int64_t)avail) flags |= kFlagOverflow;
+    const uint32_t t_end = tokens < (int64_t)a.max_tokens ? (uint32_t)tokens : a.max_tokens;
+    for (uint32_t t = t_end + tid; t < a.max_tokens; t += kTableThreads) { a.slots[t] = -1; a.positions[t] = 0; }
+    if (tid == 0) {
+        a.token_begin[a.nrequests] = (int32_t)t_end;
+        *a.free_count = (int32_t)(avail - (pages < (int64_t)avail ? (uint32_t)pages : avail));
+    }
+    if (flags) atomicOr(a.flags, flags);
+}
+
+struct ReleaseArgs {
+    const int32_t *keep;
+    uint32_t nrequests;
+    int32_t *held;
+    const int32_t *table;
+    uint32_t width;
+    int32_t *free_pages, *free_count;
+    uint32_t free_cap;
+    uint32_t *flags;
+};
+
+// The surplus pages, numbered in the order in which srs_cache_tables would have handed them out, go to the end of the free list from the
+// last to the first.
+__global__ __launch_bounds__(kTableThreads) void cache_release_kernel(const ReleaseArgs a) {
+    __shared__ uint32_t s_page[kTableThreads + 1], s_keep[kTableThreads];
+    const uint32_t tid = threadIdx.x;
+    const int32_t listed = *a.free_count;
+    const uint32_t have = listed < 0 ? 0u : (uint32_t)listed > a.free_cap ? a.free_cap : (uint32_t)listed;
+    uint32_t flags = (listed < 0 || (uint32_t)listed > a.free_cap) ? kFlagBadIndex : 0u;
+    int64_t all = 0;
+    for (uint32_t base = 0; base < a.nrequests; base += kTableThreads) {       // how many there are
+        const uint32_t r = base + tid;
+        int64_t extra = 0;
+        if (r < a.nrequests) {
+            const int32_t k = a.keep[r], h = a.held[r];
+            if (k < 0 || h < 0 || (uint32_t)(h < 0 ? 0 : h) > a.width) flags |= kFlagBadIndex;
+            const uint32_t keep = k < 0 ? 0u : (uint32_t)k, held = h < 0 ? 0u : (uint32_t)h > a.width ? a.width : (uint32_t)h;
+            extra = held > keep ? held - keep : 0;
+        }
+        int64_t x, y, n, z;
+        block_sums(extra, 0, x, y, n, z);
+        all += n;
+    }
+    const uint32_t room = a.free_cap - have;
+    if (all > (int64_t)room) flags |= kFlagOverflow;
+    int64_t before = 0;
+    for (uint32_t base = 0; base < a.nrequests; base += kTableThreads) {
+        const uint32_t r = base + tid, n = a.nrequests - base < (uint32_t)kTableThreads ? a.nrequests - base : (uint32_t)kTableThreads;
+        uint32_t extra = 0, keep = 0;
+        if (tid < n) {
+            const int32_t k = a.keep[r], h = a.held[r];
+            keep = k < 0 ? 0u : (uint32_t)k;
+            const uint32_t held = h < 0 ? 0u : (uint32_t)h > a.width ? a.width : (uint32_t)h;
+            extra = held > keep ? held - keep : 0;
+        }
+        int64_t x, y, sum, z;
+        block_sums(extra, 0, x, y, sum, z);
+        s_page[tid] = (uint32_t)x; s_keep[tid] = keep;
+        if (tid == n - 1) s_page[n] = (uint32_t)sum;
+        __syncthreads();
+        for (uint32_t k = tid; k < (uint32_t)sum; k += kTableThreads) {
+            const uint32_t q = last_at_most(s_page, n, k);
+            const int64_t to = all - 1 - (before + k);                          // places behind the list's end
+            if (to < (int64_t)room) a.free_pages[have + (uint32_t)to] = a.table[(uint64_t)(base + q) * a.width + s_keep[q] + (k - s_page[q])];
+        }
+        if (extra) a.held[r] = (int32_t)keep;
+        before += sum;
+        __syncthreads();
+    }
+    if (tid == 0) *a.free_count = (int32_t)(have + (all < (int64_t)room ? (uint32_t)all : room));
+    if (flags) atomicOr(a.flags, flags);
+}
+
+// ---- rotary positions and rows into the cache --------------------------------------------------------------------------
+
+struct RowsArg {
+    unsigned char *p;
+    int64_t token_stride, head_stride;
+    uint32_t heads;
+};
+
+struct RopeArgs {
+    RowsArg x, out;                 // srs_rope: x -> out; srs_cache_write: q -> q_out (heads 0: none)
+    RowsArg k, v;                   // srs_cache_write only
+    unsigned char *k_cache, *v_cache;
+    int64_t k_page, k_token, k_head, v_page, v_token, v_head;
+    const int64_t *slots;           // NULL: no cache
+    uint64_t places;                // pages * page
+    uint32_t page;
+    uint32_t tokens, head_dim, rot;
+    const int32_t *positions;
+    const double *inv_freq;
+    float magnitude;
+    uint32_t *flags;
+};
+
+// Sine and cosine of position * frequency.  The turns are counted in double and reduced to one there: a binary32 product is off by
+// 2^-24 of up to a million radians at far positions.  What is left, at most half a turn, is binary32.
+__device__ __forceinline__ void turn_of(int32_t position, double inv_freq, float &c, float &s) {
+    const double turns = (double)position * (inv_freq * 0.15915494309189533576888376337251436);
+    const float half_turns = (float)(2.0 * (turns - rint(turns)));
+    sincospif(half_turns, &s, &c);
+}
+
+// One thread per pair, or per element that is copied.
+template <class T, bool INTERLEAVED>
+__global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a, bool transpose) {
+    const uint32_t units = a.rot / 2 + (a.head_dim - a.rot);
+    const uint32_t heads = a.x.heads + a.k.heads + a.v.heads;
+    const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= (uint64_t)a.tokens * heads * units) return;
+    const uint32_t u = (uint32_t)(i % units), head = (uint32_t)(i / units % heads), t = (uint32_t)(i / units / heads);
+    const T *from;
+    T *to;
+    bool turned = true;
+    if (head < a.x.heads) {
+        from = (const T *)a.x.p + (int64_t)t * a.x.token_stride + (int64_t)head * a.x.head_stride;
+        to = (T *)a.out.p + (int64_t)t * a.out.token_stride + (int64_t)head * a.out.head_stride;
+    } else {
+        const int64_t slot = a.slots[t];
+        if (slot < 0 || (uint64_t)slot >= a.places) {
+            if (slot != -1) atomicOr(a.flags, kFlagBadIndex);
+            return;
+        }
+        const int64_t page = slot / a.page, place = slot % a.page;
+        if (head < a.x.heads + a.k.heads) {
+            const uint32_t h = head - a.x.heads;
+            from = (const T *)a.k.p + (int64_t)t * a.k.token_stride + (int64_t)h * a.k.head_stride;
+            to = (T *)a.k_cache + page * a.k_page + place * a.k_token + (int64_t)h * a.k_head;
+        } else {
+            const uint32_t h = head - a.x.heads - a.k.heads;
+            from = (const T *)a.v.p + (int64_t)t * a.v.token_stride + (int64_t)h * a.v.head_stride;
+            to = (T *)a.v_cache + page * a.v_page + place * a.v_token + (int64_t)h * a.v_head;
+            turned = false;
+        }
+    }
+    if (u >= a.rot / 2) {
+        const uint32_t d = a.rot + (u - a.rot / 2);
+        to[d] = from[d];
+        return;
+    }
+    const uint32_t d1 = INTERLEAVED ? 2 * u : u, d2 = INTERLEAVED ? 2 * u + 1 : u + a.rot / 2;
+    if (!turned) {
+        const T x1 = from[d1], x2 = from[d2];
+        to[d1] = x1; to[d2] = x2;
+        return;
+    }
+    float c, s;
+    turn_of(a.positions[t], a.inv_freq[u], c, s);
+    c *= a.magnitude; s *= transpose ? -a.magnitude : a.magnitude;
+    const float x1 = (float)from[d1], x2 = (float)from[d2];
+    to[d1] = (T)(x1 * c - x2 * s);
+    to[d2] = (T)(x2 * c + x1 * s);
+}
+
+}  // namespace srs

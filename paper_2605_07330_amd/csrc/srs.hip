@@ -4,9 +4,12 @@
 #include "device_guard.hpp"
 #include "scratch_array.hpp"
 #include "srs_kernels.hpp"
+#include "cache_kernels.hpp"
+#include "attention_kernels.hpp"
 
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <cstddef>
 #include <cstdlib>
 #include <cstring>
@@ -1234,6 +1237,179 @@ int srs_decode_values(srs_ctx *ctx, const uint8_t *lens, const uint8_t *low, con
     a.chunk_words = const_cast<uint32_t *>(chunk_words); a.sub = const_cast<uint16_t *>(sub); a.flags = ctx->flags;
     const uint64_t groups = (nchunk + kVcDecodeChunks - 1) / kVcDecodeChunks;
     hipLaunchKernelGGL(vc_decode_kernel, dim3((uint32_t)((uint64_t)nbuckets * groups)), dim3(kThreads), 0, st, a);
+    SRS_HIP(hipGetLastError());
+    return SRS_OK;
+}
+
+// ---------------------------------------------------------------------------------------------
+// the Rollout's key/value cache
+// ---------------------------------------------------------------------------------------------
+
+int srs_cache_tables(srs_ctx *ctx, const int32_t *start, const int32_t *count, uint32_t nrequests, uint32_t page_tokens,
+                     int32_t *held, int32_t *table, uint32_t table_width, const int32_t *free_pages, int32_t *free_count,
+                     uint32_t free_cap, int32_t *token_begin, int64_t *slots, int32_t *positions, uint64_t max_tokens, void *stream) {
+    if (!ctx || page_tokens == 0 || !token_begin || !free_count || max_tokens > kMaxIndexable || free_cap > kMaxIndexable) return SRS_ERR_INVALID;
+    if (nrequests > kMaxIndexable || (uint64_t)table_width * page_tokens > kMaxIndexable) return SRS_ERR_INVALID;
+    if (nrequests && (!start || !count || !held || (table_width && !table))) return SRS_ERR_INVALID;
+    if ((free_cap && !free_pages) || (max_tokens && (!slots || !positions))) return SRS_ERR_INVALID;
+    if (((uintptr_t)start | (uintptr_t)count | (uintptr_t)held | (uintptr_t)table | (uintptr_t)free_pages | (uintptr_t)free_count |
+         (uintptr_t)token_begin | (uintptr_t)positions) & 3u || (uintptr_t)slots & 7u)
+        return SRS_ERR_INVALID;
+    hipStream_t st = (hipStream_t)stream;
+    SRS_ON_DEVICE(ctx->device);
+    TablesArgs a{start, count, nrequests, page_tokens, held, table, table_width, free_pages, free_count, free_cap,
+                 token_begin, slots, positions, (uint32_t)max_tokens, ctx->flags};
+    hipLaunchKernelGGL(cache_tables_kernel, dim3(1), dim3(kTableThreads), 0, st, a);
+    SRS_HIP(hipGetLastError());
+    return SRS_OK;
+}
+
+int srs_cache_release(srs_ctx *ctx, const int32_t *keep, uint32_t nrequests, int32_t *held, const int32_t *table,
+                      uint32_t table_width, int32_t *free_pages, int32_t *free_count, uint32_t free_cap, void *stream) {
+    if (!ctx || !free_count || free_cap > kMaxIndexable || nrequests > kMaxIndexable || table_width > kMaxIndexable) return SRS_ERR_INVALID;
+    if (nrequests == 0) return SRS_OK;
+    if (!keep || !held || (table_width && !table) || (free_cap && !free_pages)) return SRS_ERR_INVALID;
+    if (((uintptr_t)keep | (uintptr_t)held | (uintptr_t)table | (uintptr_t)free_pages | (uintptr_t)free_count) & 3u) return SRS_ERR_INVALID;
+    hipStream_t st = (hipStream_t)stream;
+    SRS_ON_DEVICE(ctx->device);
+    ReleaseArgs a{keep, nrequests, held, table, table_width, free_pages, free_count, free_cap, ctx->flags};
+    hipLaunchKernelGGL(cache_release_kernel, dim3(1), dim3(kTableThreads), 0, st, a);
+    SRS_HIP(hipGetLastError());
+    return SRS_OK;
+}
+
+namespace {
+uint32_t elem_bytes(int dtype) { return dtype == SRS_BF16 || dtype == SRS_FP16 ? 2u : dtype == SRS_FP32 ? 4u : 0u; }
+
+bool stride_ok(int64_t s) { return s >= -(1ll << 40) && s <= (1ll << 40); }
+
+// Pointer and strides of rows of `tokens` tokens; `align` in bytes.
+bool rows_ok(const srs_rows *r, uint32_t align) {
+    return r && r->p && r->heads > 0 && r->heads <= 65536 && ((uintptr_t)r->p & (align - 1)) == 0 && stride_ok(r->token_stride) && stride_ok(r->head_stride);
+}
+
+bool cache_ok(const srs_cache *c, uint32_t align) {
+    if (!c || (c->pages && (!c->k || !c->v)) || !elem_bytes(c->dtype) || c->page_tokens == 0 || c->heads == 0 || c->heads > 65536 || c->head_dim == 0 || c->head_dim > 65536)
+        return false;
+    if (c->pages > kMaxIndexable || c->page_tokens > kMaxIndexable || (((uintptr_t)c->k | (uintptr_t)c->v) & (align - 1))) return false;
+    return stride_ok(c->k_page) && stride_ok(c->k_token) && stride_ok(c->k_head) && stride_ok(c->v_page) && stride_ok(c->v_token) && stride_ok(c->v_head);
+}
+
+RowsArg rows_arg(const srs_rows *r) { return RowsArg{(unsigned char *)r->p, r->token_stride, r->head_stride, r->heads}; }
+
+bool rotation_ok(uint32_t rot_dim, uint32_t head_dim, uint32_t flags, const int32_t *positions, const double *inv_freq, float magnitude) {
+    if (rot_dim > head_dim || (rot_dim & 1u) || (flags & ~(SRS_ROPE_INTERLEAVED | SRS_ROPE_TRANSPOSE))) return false;
+    if (rot_dim == 0) return true;
+    return positions && inv_freq && !((uintptr_t)positions & 3u) && !((uintptr_t)inv_freq & 7u) && std::isfinite(magnitude);
+}
+
+int launch_rope(const RopeArgs &a, int dtype, uint32_t flags, hipStream_t st) {
+    const uint64_t n = (uint64_t)a.tokens * (a.x.heads + a.k.heads + a.v.heads) * (a.rot / 2 + (a.head_dim - a.rot));
+    if (n == 0) return SRS_OK;
+    const uint64_t blocks = (n + 255) / 256;
+    if (blocks > 0x7fffffffull) return SRS_ERR_INVALID;
+    const bool transpose = (flags & SRS_ROPE_TRANSPOSE) != 0;
+#define SRS_ROPE_LAUNCH(T)                                                                                                       \
+    do {                                                                                                                         \
+        if (flags & SRS_ROPE_INTERLEAVED) hipLaunchKernelGGL((rope_kernel<T, true>), dim3((uint32_t)blocks), dim3(256), 0, st, a, transpose); \
+        else hipLaunchKernelGGL((rope_kernel<T, false>), dim3((uint32_t)blocks), dim3(256), 0, st, a, transpose);                 \
+    } while (0)
+    if (dtype == SRS_BF16) SRS_ROPE_LAUNCH(__bf16);
+    else if (dtype == SRS_FP16) SRS_ROPE_LAUNCH(_Float16);
+    else SRS_ROPE_LAUNCH(float);
+#undef SRS_ROPE_LAUNCH
+    SRS_HIP(hipGetLastError());
+    return SRS_OK;
+}
+}  // namespace
+
+int srs_rope(srs_ctx *ctx, int dtype, const srs_rows *x, const srs_rows *out, uint64_t tokens, uint32_t head_dim,
+             const int32_t *positions, const double *inv_freq, uint32_t rot_dim, uint32_t flags, float magnitude, void *stream) {
+    const uint32_t size = elem_bytes(dtype);
+    if (!ctx || !size || head_dim == 0 || head_dim > 65536 || tokens > kMaxIndexable) return SRS_ERR_INVALID;
+    if (!rotation_ok(rot_dim, head_dim, flags, positions, inv_freq, magnitude)) {
+        if (tokens || rot_dim > head_dim || (rot_dim & 1u)) return SRS_ERR_INVALID;
+    }
+    if (tokens == 0) return SRS_OK;
+    if (!rows_ok(x, size) || !rows_ok(out, size) || x->heads != out->heads) return SRS_ERR_INVALID;
+    hipStream_t st = (hipStream_t)stream;
+    SRS_ON_DEVICE(ctx->device);
+    RopeArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.x = rows_arg(x); a.out = rows_arg(out);
+    a.tokens = (uint32_t)tokens; a.head_dim = head_dim; a.rot = rot_dim; a.page = 1;
+    a.positions = positions; a.inv_freq = inv_freq; a.magnitude = magnitude; a.flags = ctx->flags;
+    return launch_rope(a, dtype, flags, st);
+}
+
+int srs_cache_write(srs_ctx *ctx, const srs_cache *cache, const srs_rows *k, const srs_rows *v, uint64_t tokens,
+                    const int64_t *slots, const srs_rows *q, const srs_rows *q_out, const int32_t *positions, const double *inv_freq,
+                    uint32_t rot_dim, uint32_t flags, float magnitude, void *stream) {
+    if (!ctx || !cache || tokens > kMaxIndexable) return SRS_ERR_INVALID;
+    const uint32_t size = elem_bytes(cache->dtype);
+    if (!size || !cache_ok(cache, size)) return SRS_ERR_INVALID;
+    if (tokens == 0) return SRS_OK;
+    if (!rotation_ok(rot_dim, cache->head_dim, flags, positions, inv_freq, magnitude)) return SRS_ERR_INVALID;
+    if (!rows_ok(k, size) || !rows_ok(v, size) || k->heads != cache->heads || v->heads != cache->heads || !slots || ((uintptr_t)slots & 7u)) return SRS_ERR_INVALID;
+    const bool queries = rot_dim > 0 && q;
+    if (queries && (!rows_ok(q, size) || !rows_ok(q_out, size) || q->heads != q_out->heads)) return SRS_ERR_INVALID;
+    hipStream_t st = (hipStream_t)stream;
+    SRS_ON_DEVICE(ctx->device);
+    RopeArgs a;
+    std::memset(&a, 0, sizeof(a));
+    if (queries) { a.x = rows_arg(q); a.out = rows_arg(q_out); }
+    a.k = rows_arg(k); a.v = rows_arg(v);
+    a.k_cache = (unsigned char *)cache->k; a.v_cache = (unsigned char *)cache->v;
+    a.k_page = cache->k_page; a.k_token = cache->k_token; a.k_head = cache->k_head;
+    a.v_page = cache->v_page; a.v_token = cache->v_token; a.v_head = cache->v_head;
+    a.slots = slots; a.places = (uint64_t)cache->pages * cache->page_tokens; a.page = cache->page_tokens;
+    a.tokens = (uint32_t)tokens; a.head_dim = cache->head_dim; a.rot = rot_dim;
+    a.positions = positions; a.inv_freq = inv_freq; a.magnitude = magnitude; a.flags = ctx->flags;
+    return launch_rope(a, cache->dtype, flags, st);
+}
+
+uint64_t srs_cache_attention_workspace(uint32_t nrequests, uint64_t tokens, uint32_t q_heads, uint32_t kv_heads, uint32_t head_dim,
+                                       uint32_t table_width, uint32_t page_tokens, uint32_t window, uint32_t sinks,
+                                       uint64_t most_tokens, uint64_t most_keys) {
+    (void)nrequests; (void)tokens; (void)q_heads; (void)kv_heads; (void)head_dim; (void)table_width; (void)page_tokens;
+    (void)window; (void)sinks; (void)most_tokens; (void)most_keys;
+    return 0;
+}
+
+int srs_cache_attention(srs_ctx *ctx, const srs_cache *cache, const srs_rows *q, const srs_rows *out, float *lse, uint64_t tokens,
+                        const int32_t *token_begin, const int32_t *start, const int32_t *table, uint32_t table_width,
+                        uint32_t nrequests, float scale, uint32_t flags, uint32_t window, uint32_t sinks, uint64_t most_tokens,
+                        uint64_t most_keys, void *workspace, uint64_t workspace_bytes, void *stream) {
+    if (!ctx || !cache || tokens > kMaxIndexable || nrequests > kMaxIndexable || (flags & ~SRS_ATTN_FULL) || !std::isfinite(scale)) return SRS_ERR_INVALID;
+    if ((cache->dtype != SRS_BF16 && cache->dtype != SRS_FP16) || !cache_ok(cache, 16)) return SRS_ERR_INVALID;
+    if (cache->head_dim > 256 || (cache->head_dim & 7u) || window > kMaxIndexable || sinks > kMaxIndexable || (sinks && !window)) return SRS_ERR_INVALID;
+    if ((flags & SRS_ATTN_FULL) && (window || sinks)) return SRS_ERR_INVALID;
+    if (((cache->k_page | cache->k_token | cache->k_head | cache->v_page | cache->v_token | cache->v_head) & 7) != 0) return SRS_ERR_INVALID;
+    if (tokens == 0 || nrequests == 0) return SRS_OK;
+    if (!rows_ok(q, 16) || !rows_ok(out, 16) || q->heads != out->heads || q->heads % cache->heads) return SRS_ERR_INVALID;
+    if (((q->token_stride | q->head_stride | out->token_stride | out->head_stride) & 7) != 0) return SRS_ERR_INVALID;
+    if (!token_begin || !start || (table_width && !table) || (uint64_t)table_width * cache->page_tokens > kMaxIndexable) return SRS_ERR_INVALID;
+    if (((uintptr_t)token_begin | (uintptr_t)start | (uintptr_t)table | (uintptr_t)lse) & 3u) return SRS_ERR_INVALID;
+    if (workspace_bytes < srs_cache_attention_workspace(nrequests, tokens, q->heads, cache->heads, cache->head_dim, table_width,
+                                                        cache->page_tokens, window, sinks, most_tokens, most_keys)) return SRS_ERR_INVALID;
+    (void)workspace;
+    if (tokens * q->heads > 0x7fffffffull) return SRS_ERR_INVALID;
+    hipStream_t st = (hipStream_t)stream;
+    SRS_ON_DEVICE(ctx->device);
+    AttnArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.q = (const unsigned char *)q->p; a.out = (unsigned char *)out->p; a.lse = lse;
+    a.k = (const unsigned char *)cache->k; a.v = (const unsigned char *)cache->v;
+    a.q_token = q->token_stride; a.q_head = q->head_stride; a.o_token = out->token_stride; a.o_head = out->head_stride;
+    a.k_page = cache->k_page; a.k_token = cache->k_token; a.k_head = cache->k_head;
+    a.v_page = cache->v_page; a.v_token = cache->v_token; a.v_head = cache->v_head;
+    a.token_begin = token_begin; a.start = start; a.table = table;
+    a.tokens = (uint32_t)tokens; a.nrequests = nrequests; a.width = table_width; a.page = cache->page_tokens; a.pages = cache->pages;
+    a.heads = q->heads; a.kv_heads = cache->heads; a.head_dim = cache->head_dim;
+    a.window = window; a.sinks = sinks; a.scale = scale; a.full = (flags & SRS_ATTN_FULL) != 0; a.flags = ctx->flags;
+    const dim3 grid((uint32_t)(tokens * q->heads));
+    if (cache->dtype == SRS_BF16) hipLaunchKernelGGL((attention_rows_kernel<__bf16>), grid, dim3(64), 0, st, a);
+    else hipLaunchKernelGGL((attention_rows_kernel<_Float16>), grid, dim3(64), 0, st, a);
     SRS_HIP(hipGetLastError());
     return SRS_OK;
 }

@@ -10,6 +10,7 @@ Importing this module fails loudly when the library has not been built
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 import warnings
 from typing import List, Optional, Sequence
@@ -41,7 +42,11 @@ EXPORTS = [
     "srs_value_chunks", "srs_encode_values", "srs_decode_values",
     "srs_extract_u8", "srs_apply_u8", "srs_extract_multi_u8", "srs_apply_multi_u8", "srs_tensor_indices",
     "srs_extract_noalloc",
+    "srs_cache_tables", "srs_cache_release", "srs_rope", "srs_cache_write", "srs_cache_attention", "srs_cache_attention_workspace",
 ]
+BF16, FP16, FP32 = 0, 1, 2
+ROPE_INTERLEAVED, ROPE_TRANSPOSE, ATTN_FULL = 1, 2, 1
+_DTYPES = {torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32}
 
 
 class TensorPair(C.Structure):
@@ -50,6 +55,16 @@ class TensorPair(C.Structure):
 
 class Tensor(C.Structure):
     _fields_ = [("weights", C.c_void_p)]
+
+
+class Rows(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("heads", C.c_uint32), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class Cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("dtype", C.c_int), ("pages", C.c_uint32), ("page_tokens", C.c_uint32),
+                ("heads", C.c_uint32), ("head_dim", C.c_uint32), ("k_page", C.c_int64), ("k_token", C.c_int64), ("k_head", C.c_int64),
+                ("v_page", C.c_int64), ("v_token", C.c_int64), ("v_head", C.c_int64)]
 
 
 _vp, _u64, _u32p = C.c_void_p, C.c_uint64, C.POINTER(C.c_uint32)
@@ -97,9 +112,18 @@ _lib.srs_decode_values.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, C.c_uint32
 _lib.srs_route.argtypes = [_vp, _vp, C.c_uint32, _u64, _u64, _u64, C.c_uint32, C.c_uint32, _vp, _vp, _vp, _vp, _vp]
 _lib.srs_pack_dense_multi.argtypes = [_vp, _vp, C.POINTER(TensorPair), _vp, _vp, C.c_uint32, _vp, _vp]
 _lib.srs_unpack_dense_multi.argtypes = [_vp, _vp, C.POINTER(Tensor), _vp, _vp, C.c_uint32, _vp, _vp]
+_u32, _rows = C.c_uint32, C.POINTER(Rows)
+_lib.srs_cache_tables.argtypes = [_vp, _vp, _vp, _u32, _u32, _vp, _vp, _u32, _vp, _vp, _u32, _vp, _vp, _vp, _u64, _vp]
+_lib.srs_cache_release.argtypes = [_vp, _vp, _u32, _vp, _vp, _u32, _vp, _vp, _u32, _vp]
+_lib.srs_rope.argtypes = [_vp, C.c_int, _rows, _rows, _u64, _u32, _vp, _vp, _u32, _u32, C.c_float, _vp]
+_lib.srs_cache_write.argtypes = [_vp, C.POINTER(Cache), _rows, _rows, _u64, _vp, _rows, _rows, _vp, _vp, _u32, _u32, C.c_float, _vp]
+_lib.srs_cache_attention_workspace.argtypes = [_u32, _u64, _u32, _u32, _u32, _u32, _u32, _u32, _u32, _u64, _u64]
+_lib.srs_cache_attention_workspace.restype = _u64
+_lib.srs_cache_attention.argtypes = [_vp, C.POINTER(Cache), _rows, _rows, _vp, _u64, _vp, _vp, _vp, _u32, _u32, C.c_float, _u32, _u32,
+                                     _u32, _u64, _u64, _vp, _u64, _vp]
 for _n in EXPORTS:
     if _n not in ("srs_strerror", "srs_stream_probe_sink_words", "srs_anchor_count", "srs_bitmap_words",
-                  "srs_value_chunks"):
+                  "srs_value_chunks", "srs_cache_attention_workspace"):
         getattr(_lib, _n).restype = C.c_int
 
 
@@ -608,6 +632,132 @@ class Context:
         _check(_lib.srs_unpack_dense_multi(self._h, plan._h, tensors, dense_bucket.data_ptr(), n_dense.data_ptr(),
                                            max_dense, dense.data_ptr(), _stream_ptr(stream)), "srs_unpack_dense_multi")
 
+    # ---- the Rollout's key/value cache ------------------------------------------------------
+    def _here(self, t: torch.Tensor, what: str, dtype: torch.dtype, at_least: int = 0) -> int:
+        """Address of a contiguous tensor of the given type on this context's device."""
+        if not (isinstance(t, torch.Tensor) and t.is_cuda and t.device.index == self.device and t.dtype == dtype and t.is_contiguous()
+                and t.numel() >= at_least):
+            raise TypeError(f"{what}: expected a contiguous {dtype} tensor of at least {at_least} elements on cuda:{self.device}")
+        return t.data_ptr()
+
+    def _stream(self, stream: Optional[torch.cuda.Stream]) -> int:
+        """The given stream, or the current one of this context's device (whatever device is current)."""
+        if stream is None:
+            return _raw_stream(self.device) if _raw_stream is not None else int(torch.cuda.current_stream(self.device).cuda_stream)
+        if stream.device.index != self.device:
+            raise TypeError(f"stream: expected one of cuda:{self.device}")
+        return int(stream.cuda_stream)
+
+    def _rows(self, t: torch.Tensor, what: str, tokens: int, head_dim: int, dtype: torch.dtype) -> Rows:
+        if not (isinstance(t, torch.Tensor) and t.is_cuda and t.device.index == self.device and t.dtype == dtype and t.dim() == 3
+                and t.shape[0] == tokens and t.shape[2] == head_dim and (head_dim == 1 or t.stride(2) == 1)):
+            raise TypeError(f"{what}: expected a {dtype} tensor [{tokens}, heads, {head_dim}] on cuda:{self.device} with its last dimension dense")
+        return Rows(t.data_ptr(), t.shape[1], t.stride(0), t.stride(1))
+
+    def _cache(self, k_cache: torch.Tensor, v_cache: torch.Tensor) -> Cache:
+        for t, what in ((k_cache, "k_cache"), (v_cache, "v_cache")):
+            if not (isinstance(t, torch.Tensor) and t.is_cuda and t.device.index == self.device and t.dim() == 4 and t.dtype in _DTYPES
+                    and (t.shape[3] == 1 or t.stride(3) == 1)):
+                raise TypeError(f"{what}: expected a tensor [pages, page_tokens, heads, head_dim] on cuda:{self.device} with its last dimension dense")
+        if k_cache.shape != v_cache.shape or k_cache.dtype != v_cache.dtype:
+            raise ValueError("k_cache and v_cache differ in shape or type")
+        pages, page, heads, d = k_cache.shape
+        return Cache(k_cache.data_ptr(), v_cache.data_ptr(), _DTYPES[k_cache.dtype], pages, page, heads, d, k_cache.stride(0), k_cache.stride(1),
+                     k_cache.stride(2), v_cache.stride(0), v_cache.stride(1), v_cache.stride(2))
+
+    def cache_tables(self, start: torch.Tensor, count: torch.Tensor, page_tokens: int, held: torch.Tensor, table: torch.Tensor,
+                     free_pages: torch.Tensor, free_count: torch.Tensor, token_begin: torch.Tensor, slots: torch.Tensor,
+                     positions: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
+        """Block tables, slots and positions of the new tokens of start.numel() requests; table is [requests, width], slots and
+        positions are as long as the (padded) batch.  held, table, free_count and the last three are written."""
+        i32, n = torch.int32, start.numel()
+        if table.dim() != 2 or table.shape[0] != n:
+            raise TypeError(f"table: expected [{n}, width]")
+        if positions.numel() < slots.numel():
+            raise ValueError("positions is shorter than slots")
+        _not_negative("srs_cache_tables", page_tokens)
+        _check(_lib.srs_cache_tables(self._h, self._here(start, "start", i32), self._here(count, "count", i32, n), n, page_tokens,
+                                     self._here(held, "held", i32, n), self._here(table, "table", i32), table.shape[1],
+                                     self._here(free_pages, "free_pages", i32), self._here(free_count, "free_count", i32, 1),
+                                     free_pages.numel(), self._here(token_begin, "token_begin", i32, n + 1),
+                                     self._here(slots, "slots", torch.int64), self._here(positions, "positions", i32), slots.numel(),
+                                     self._stream(stream)), "srs_cache_tables")
+
+    def cache_release(self, keep: torch.Tensor, held: torch.Tensor, table: torch.Tensor, free_pages: torch.Tensor,
+                      free_count: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
+        """Requests keep their first keep[r] pages, the others go back to the free list."""
+        i32, n = torch.int32, keep.numel()
+        if table.dim() != 2 or table.shape[0] != n:
+            raise TypeError(f"table: expected [{n}, width]")
+        _check(_lib.srs_cache_release(self._h, self._here(keep, "keep", i32), n, self._here(held, "held", i32, n),
+                                      self._here(table, "table", i32), table.shape[1], self._here(free_pages, "free_pages", i32),
+                                      self._here(free_count, "free_count", i32, 1), free_pages.numel(), self._stream(stream)),
+               "srs_cache_release")
+
+    def rope(self, x: torch.Tensor, out: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor, interleaved: bool = False,
+             magnitude: float = 1.0, transpose: bool = False, stream: Optional[torch.cuda.Stream] = None) -> None:
+        """Rotary positions on x [tokens, heads, head_dim] into out (which may be x); transpose: the gradient.  inv_freq: float64."""
+        if x.dim() != 3 or x.dtype not in _DTYPES:
+            raise TypeError("x: expected a bfloat16, float16 or float32 tensor [tokens, heads, head_dim]")
+        T, heads, d = x.shape
+        if out.shape != x.shape:
+            raise ValueError("x and out differ in shape")
+        rx, ro = self._rows(x, "x", T, d, x.dtype), self._rows(out, "out", T, d, x.dtype)
+        flags = (ROPE_INTERLEAVED if interleaved else 0) | (ROPE_TRANSPOSE if transpose else 0)
+        _check(_lib.srs_rope(self._h, _DTYPES[x.dtype], C.byref(rx), C.byref(ro), T, d, self._here(positions, "positions", torch.int32, T),
+                             self._here(inv_freq, "inv_freq", torch.float64), 2 * inv_freq.numel(), flags, magnitude,
+                             self._stream(stream)), "srs_rope")
+
+    def cache_write(self, k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, slots: torch.Tensor,
+                    q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+                    inv_freq: Optional[torch.Tensor] = None, interleaved: bool = False, magnitude: float = 1.0,
+                    stream: Optional[torch.cuda.Stream] = None) -> None:
+        """Rows of k and v [tokens, heads, head_dim] into the cache at slots; with inv_freq k is turned on the way, and q into q_out."""
+        cache = self._cache(k_cache, v_cache)
+        dt, T, d = k_cache.dtype, slots.numel(), k_cache.shape[3]
+        rk, rv = self._rows(k, "k", T, d, dt), self._rows(v, "v", T, d, dt)
+        rot = 0 if inv_freq is None else 2 * inv_freq.numel()
+        rq = ro = pos = freq = None
+        if rot:
+            if positions is None:
+                raise TypeError("positions: needed with inv_freq")
+            pos, freq = self._here(positions, "positions", torch.int32, T), self._here(inv_freq, "inv_freq", torch.float64)
+        if q is not None:
+            if not rot or q_out is None:
+                raise TypeError("q: needs q_out, positions and inv_freq")
+            rq, ro = C.byref(self._rows(q, "q", T, d, dt)), C.byref(self._rows(q_out, "q_out", T, d, dt))
+        _check(_lib.srs_cache_write(self._h, C.byref(cache), C.byref(rk), C.byref(rv), T, self._here(slots, "slots", torch.int64), rq, ro, pos,
+                                    freq, rot, ROPE_INTERLEAVED if interleaved else 0, magnitude, self._stream(stream)), "srs_cache_write")
+
+    def cache_attention(self, q: torch.Tensor, out: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor,
+                        token_begin: torch.Tensor, start: torch.Tensor, scale: Optional[float] = None, causal: bool = True,
+                        window: int = 0, sinks: int = 0, lse: Optional[torch.Tensor] = None, most_tokens: int = 0, most_keys: int = 0,
+                        workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+        """Attention of the new tokens q [tokens, heads, head_dim] over the paged cache.  scale: 1 / sqrt(head_dim) by default.
+        most_tokens, most_keys: the most new tokens and keys of any request, as far as known.  workspace: device memory of
+        attention_workspace() bytes; without it the call takes what it needs from torch, on its stream."""
+        cache = self._cache(k_cache, v_cache)
+        T, d, n, i32 = q.shape[0], k_cache.shape[3], start.numel(), torch.int32
+        rq, ro = self._rows(q, "q", T, d, k_cache.dtype), self._rows(out, "out", T, d, k_cache.dtype)
+        if table.dim() != 2 or table.shape[0] != n:
+            raise TypeError(f"table: expected [{n}, width]")
+        _not_negative("srs_cache_attention", window, sinks, most_tokens, most_keys)
+        need = _lib.srs_cache_attention_workspace(n, T, rq.heads, cache.heads, d, table.shape[1], cache.page_tokens, window, sinks,
+                                                  most_tokens, most_keys)
+        if need and workspace is None:
+            with torch.cuda.device(self.device), torch.cuda.stream(stream):
+                workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        ws = nbytes = 0
+        if workspace is not None:
+            if not (workspace.is_cuda and workspace.device.index == self.device and workspace.is_contiguous()):
+                raise TypeError(f"workspace: expected a contiguous tensor on cuda:{self.device}")
+            ws, nbytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        _check(_lib.srs_cache_attention(self._h, C.byref(cache), C.byref(rq), C.byref(ro), None if lse is None else self._here(lse, "lse", torch.float32, T * rq.heads),
+                                        T, self._here(token_begin, "token_begin", i32, n + 1), self._here(start, "start", i32),
+                                        self._here(table, "table", i32), table.shape[1], n, d ** -0.5 if scale is None else scale,
+                                        0 if causal else ATTN_FULL, window, sinks, most_tokens, most_keys, ws, nbytes,
+                                        self._stream(stream)), "srs_cache_attention")
+
     # ---- measurement aid ------------------------------------------------------------------
     def stream_probe(self, a: torch.Tensor, b: torch.Tensor, sink: torch.Tensor,
                      stream: Optional[torch.cuda.Stream] = None) -> None:
@@ -618,6 +768,41 @@ class Context:
             raise ValueError("sink too small")
         _check(_lib.srs_stream_probe(self._h, a.data_ptr(), b.data_ptr(), nbytes, sink.data_ptr(), _stream_ptr(stream)),
                "srs_stream_probe")
+
+
+def attention_workspace(nrequests: int, tokens: int, q_heads: int, kv_heads: int, head_dim: int, table_width: int, page_tokens: int,
+                        window: int = 0, sinks: int = 0, most_tokens: int = 0, most_keys: int = 0) -> int:
+    """Bytes of workspace that cache_attention needs for these sizes."""
+    return int(_lib.srs_cache_attention_workspace(nrequests, tokens, q_heads, kv_heads, head_dim, table_width, page_tokens, window, sinks,
+                                                  most_tokens, most_keys))
+
+
+def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, original_context: int = 0,
+                     fast_turns: float = 32.0, slow_turns: float = 1.0, device=None) -> tuple:
+    """(inv_freq, magnitude) for ``Context.rope`` and ``Context.cache_write``: angle per position of each of the rot_dim / 2 pairs, float64.
+
+    ``none``    base ** (-2 i / rot_dim)
+    ``linear``  the same over ``factor``: positions run ``factor`` times slower
+    ``base``    the base times factor ** (rot_dim / (rot_dim - 2)): the slowest pair runs ``factor`` times slower, the fastest as before
+    ``parts``   pairs that turn at least ``fast_turns`` times over ``original_context`` positions as before, those that turn at most
+                ``slow_turns`` times ``factor`` times slower, a linear mixture between; magnitude 0.1 log(factor) + 1
+    """
+    if rot_dim <= 0 or rot_dim % 2 or base <= 0 or factor < 1:
+        raise ValueError("rot_dim: even and positive; base: positive; factor: at least 1")
+    i = torch.arange(0, rot_dim, 2, dtype=torch.float64)
+    if scaling == "base":
+        base = base * factor ** (rot_dim / max(1, rot_dim - 2))
+    inv, magnitude = base ** (-i / rot_dim), 1.0
+    if scaling == "linear":
+        inv = inv / factor
+    elif scaling == "parts":
+        if original_context <= 0 or fast_turns <= slow_turns:
+            raise ValueError("parts: needs original_context, and fast_turns above slow_turns")
+        kept = ((inv * original_context / (2 * math.pi) - slow_turns) / (fast_turns - slow_turns)).clamp(0, 1)
+        inv, magnitude = inv * (kept + (1 - kept) / factor), 0.1 * math.log(factor) + 1.0
+    elif scaling not in ("none", "base"):
+        raise ValueError(f"scaling {scaling!r}: none, linear, base or parts")
+    return inv.to(device), magnitude
 
 
 def value_chunks(cap: int) -> int:
