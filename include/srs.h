@@ -445,6 +445,7 @@ int srs_cache_write(srs_ctx *ctx, const srs_cache *cache, const srs_rows *k, con
  * beyond table_width pages are hidden and raise it too.
  * most_tokens and most_keys: the largest count and the largest number of keys of a request, as far as the caller knows (0: unknown).
  * They choose how the work is split, nothing else.
+ * table_width * page_tokens is at most 2^30, tokens * q->heads below 2^31.
  * workspace: device memory, 16-byte aligned, of at least srs_cache_attention_workspace bytes for the same sizes (0 bytes: none is needed);
  * written and read by this call only, so calls that cannot overlap may share one.
  */

@@ -624,6 +624,118 @@ int extract_multi(srs_ctx *ctx, srs_plan *plan, const srs_tensor_pair *t,
 }
 }  // namespace
 
+namespace {
+uint32_t elem_bytes(int dtype) { return dtype == SRS_BF16 || dtype == SRS_FP16 ? 2u : dtype == SRS_FP32 ? 4u : 0u; }
+
+bool stride_ok(int64_t s) { return s >= -(1ll << 40) && s <= (1ll << 40); }
+
+// Pointer and strides of rows of `tokens` tokens; `align` in bytes.
+bool rows_ok(const srs_rows *r, uint32_t align) {
+    return r && r->p && r->heads > 0 && r->heads <= 65536 && ((uintptr_t)r->p & (align - 1)) == 0 && stride_ok(r->token_stride) && stride_ok(r->head_stride);
+}
+
+bool cache_ok(const srs_cache *c, uint32_t align) {
+    if (!c || (c->pages && (!c->k || !c->v)) || !elem_bytes(c->dtype) || c->page_tokens == 0 || c->heads == 0 || c->heads > 65536 || c->head_dim == 0 || c->head_dim > 65536)
+        return false;
+    if (c->pages > kMaxIndexable || c->page_tokens > kMaxIndexable || (((uintptr_t)c->k | (uintptr_t)c->v) & (align - 1))) return false;
+    return stride_ok(c->k_page) && stride_ok(c->k_token) && stride_ok(c->k_head) && stride_ok(c->v_page) && stride_ok(c->v_token) && stride_ok(c->v_head);
+}
+
+RowsArg rows_arg(const srs_rows *r) { return RowsArg{(unsigned char *)r->p, r->token_stride, r->head_stride, r->heads}; }
+
+bool rotation_ok(uint32_t rot_dim, uint32_t head_dim, uint32_t flags, const int32_t *positions, const double *inv_freq, float magnitude) {
+    if (rot_dim > head_dim || (rot_dim & 1u) || (flags & ~(SRS_ROPE_INTERLEAVED | SRS_ROPE_TRANSPOSE))) return false;
+    if (rot_dim == 0) return true;
+    return positions && inv_freq && !((uintptr_t)positions & 3u) && !((uintptr_t)inv_freq & 7u) && std::isfinite(magnitude);
+}
+
+int launch_rope(const RopeArgs &a, int dtype, uint32_t flags, hipStream_t st) {
+    const uint64_t n = (uint64_t)a.tokens * (a.x.heads + a.k.heads + a.v.heads) * (a.rot / 2 + (a.head_dim - a.rot));
+    if (n == 0) return SRS_OK;
+    const uint64_t blocks = (n + 255) / 256;
+    if (blocks > 0x7fffffffull) return SRS_ERR_INVALID;
+    const bool transpose = (flags & SRS_ROPE_TRANSPOSE) != 0;
+#define SRS_ROPE_LAUNCH(T)                                                                                                       \
+    do {                                                                                                                         \
+        if (flags & SRS_ROPE_INTERLEAVED) hipLaunchKernelGGL((rope_kernel<T, true>), dim3((uint32_t)blocks), dim3(256), 0, st, a, transpose); \
+        else hipLaunchKernelGGL((rope_kernel<T, false>), dim3((uint32_t)blocks), dim3(256), 0, st, a, transpose);                 \
+    } while (0)
+    if (dtype == SRS_BF16) SRS_ROPE_LAUNCH(__bf16);
+    else if (dtype == SRS_FP16) SRS_ROPE_LAUNCH(_Float16);
+    else SRS_ROPE_LAUNCH(float);
+#undef SRS_ROPE_LAUNCH
+    SRS_HIP(hipGetLastError());
+    return SRS_OK;
+}
+}  // namespace
+
+namespace {
+// How the attention of one call is laid out.
+struct AttnPlan {
+    uint32_t block, head_blocks, tile_tokens, tiles, splits, split_tiles;
+    uint64_t workspace;
+};
+
+constexpr uint64_t kMaxKeys = 1ull << 30;              // of one request
+
+// Workgroups that a launch should have where rows are few: three of them fit a CU, and four rounds even out requests of unlike length.
+constexpr uint64_t kAttnWorkgroups = 256 * 3 * 4;
+constexpr uint32_t kLeastSplitTiles = 2;
+
+AttnPlan attention_plan(uint32_t nrequests, uint64_t tokens, uint32_t q_heads, uint32_t kv_heads, uint32_t head_dim, uint32_t table_width,
+                        uint32_t page_tokens, uint32_t window, uint32_t sinks, uint64_t most_tokens, uint64_t most_keys) {
+    AttnPlan p;
+    const uint32_t group = q_heads / kv_heads;
+    p.head_blocks = (group + 15) / 16;
+    p.block = (group + p.head_blocks - 1) / p.head_blocks;
+    p.tile_tokens = 16 / p.block;
+    p.tiles = (uint32_t)(tokens / p.tile_tokens + nrequests);
+    uint64_t keys = (uint64_t)table_width * page_tokens;
+    if (most_keys && most_keys < keys) keys = most_keys;
+    uint64_t key_tiles = (keys + kNarrowKeys - 1) / kNarrowKeys;
+    if (window) {
+        const uint64_t seen = (sinks + kNarrowKeys - 1) / kNarrowKeys + ((uint64_t)window + p.tile_tokens + kNarrowKeys - 1) / kNarrowKeys + 1;
+        if (seen < key_tiles) key_tiles = seen;
+    }
+    const uint64_t busy = tokens < p.tiles ? tokens : p.tiles;             // tiles that hold something, at most
+    const uint64_t units = busy * kv_heads * p.head_blocks;
+    uint64_t each = (units * key_tiles + kAttnWorkgroups - 1) / kAttnWorkgroups;
+    each = each < kLeastSplitTiles ? kLeastSplitTiles : each;
+    uint64_t splits = (key_tiles + each - 1) / each;
+    if (splits < 1) splits = 1;
+    p.split_tiles = (uint32_t)each; p.splits = (uint32_t)splits;
+    p.workspace = splits > 1 ? tokens * q_heads * 4 * (splits * (head_dim + 1) + 1) : 0;
+    (void)most_tokens;
+    return p;
+}
+
+// Pages that hold whole blocks of 16 keys, whose rows a 32-bit offset spans: addresses are then scalar but for that offset.
+bool in_blocks(const srs_cache *c) {
+    const int64_t most = 1ll << 26;
+    return c->page_tokens % 16 == 0 && c->k_token >= 0 && c->k_token <= most && c->v_token >= 0 && c->v_token <= most;
+}
+
+template <class T, int DP>
+int launch_attention(const AttnArgs &a, bool blocks, uint32_t grid, hipStream_t st) {
+    if (blocks && a.head_dim == DP) hipLaunchKernelGGL((attention_narrow_kernel<T, DP, true, true>), dim3(grid), dim3(256), 0, st, a);
+    else if (blocks) hipLaunchKernelGGL((attention_narrow_kernel<T, DP, true, false>), dim3(grid), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((attention_narrow_kernel<T, DP, false, false>), dim3(grid), dim3(256), 0, st, a);
+    SRS_HIP(hipGetLastError());
+    if (a.splits > 1) {
+        hipLaunchKernelGGL((attention_join_kernel<T>), dim3((uint32_t)(((uint64_t)a.tokens * a.heads + 3) / 4)), dim3(256), 0, st, a);
+        SRS_HIP(hipGetLastError());
+    }
+    return SRS_OK;
+}
+
+template <class T>
+int launch_attention(const AttnArgs &a, bool blocks, uint32_t grid, hipStream_t st) {
+    if (a.head_dim <= 64) return launch_attention<T, 64>(a, blocks, grid, st);
+    if (a.head_dim <= 128) return launch_attention<T, 128>(a, blocks, grid, st);
+    return launch_attention<T, 256>(a, blocks, grid, st);
+}
+}  // namespace
+
 extern "C" {
 
 int srs_version(void) { return 100; }
@@ -1278,50 +1390,6 @@ int srs_cache_release(srs_ctx *ctx, const int32_t *keep, uint32_t nrequests, int
     return SRS_OK;
 }
 
-namespace {
-uint32_t elem_bytes(int dtype) { return dtype == SRS_BF16 || dtype == SRS_FP16 ? 2u : dtype == SRS_FP32 ? 4u : 0u; }
-
-bool stride_ok(int64_t s) { return s >= -(1ll << 40) && s <= (1ll << 40); }
-
-// Pointer and strides of rows of `tokens` tokens; `align` in bytes.
-bool rows_ok(const srs_rows *r, uint32_t align) {
-    return r && r->p && r->heads > 0 && r->heads <= 65536 && ((uintptr_t)r->p & (align - 1)) == 0 && stride_ok(r->token_stride) && stride_ok(r->head_stride);
-}
-
-bool cache_ok(const srs_cache *c, uint32_t align) {
-    if (!c || (c->pages && (!c->k || !c->v)) || !elem_bytes(c->dtype) || c->page_tokens == 0 || c->heads == 0 || c->heads > 65536 || c->head_dim == 0 || c->head_dim > 65536)
-        return false;
-    if (c->pages > kMaxIndexable || c->page_tokens > kMaxIndexable || (((uintptr_t)c->k | (uintptr_t)c->v) & (align - 1))) return false;
-    return stride_ok(c->k_page) && stride_ok(c->k_token) && stride_ok(c->k_head) && stride_ok(c->v_page) && stride_ok(c->v_token) && stride_ok(c->v_head);
-}
-
-RowsArg rows_arg(const srs_rows *r) { return RowsArg{(unsigned char *)r->p, r->token_stride, r->head_stride, r->heads}; }
-
-bool rotation_ok(uint32_t rot_dim, uint32_t head_dim, uint32_t flags, const int32_t *positions, const double *inv_freq, float magnitude) {
-    if (rot_dim > head_dim || (rot_dim & 1u) || (flags & ~(SRS_ROPE_INTERLEAVED | SRS_ROPE_TRANSPOSE))) return false;
-    if (rot_dim == 0) return true;
-    return positions && inv_freq && !((uintptr_t)positions & 3u) && !((uintptr_t)inv_freq & 7u) && std::isfinite(magnitude);
-}
-
-int launch_rope(const RopeArgs &a, int dtype, uint32_t flags, hipStream_t st) {
-    const uint64_t n = (uint64_t)a.tokens * (a.x.heads + a.k.heads + a.v.heads) * (a.rot / 2 + (a.head_dim - a.rot));
-    if (n == 0) return SRS_OK;
-    const uint64_t blocks = (n + 255) / 256;
-    if (blocks > 0x7fffffffull) return SRS_ERR_INVALID;
-    const bool transpose = (flags & SRS_ROPE_TRANSPOSE) != 0;
-#define SRS_ROPE_LAUNCH(T)                                                                                                       \
-    do {                                                                                                                         \
-        if (flags & SRS_ROPE_INTERLEAVED) hipLaunchKernelGGL((rope_kernel<T, true>), dim3((uint32_t)blocks), dim3(256), 0, st, a, transpose); \
-        else hipLaunchKernelGGL((rope_kernel<T, false>), dim3((uint32_t)blocks), dim3(256), 0, st, a, transpose);                 \
-    } while (0)
-    if (dtype == SRS_BF16) SRS_ROPE_LAUNCH(__bf16);
-    else if (dtype == SRS_FP16) SRS_ROPE_LAUNCH(_Float16);
-    else SRS_ROPE_LAUNCH(float);
-#undef SRS_ROPE_LAUNCH
-    SRS_HIP(hipGetLastError());
-    return SRS_OK;
-}
-}  // namespace
 
 int srs_rope(srs_ctx *ctx, int dtype, const srs_rows *x, const srs_rows *out, uint64_t tokens, uint32_t head_dim,
              const int32_t *positions, const double *inv_freq, uint32_t rot_dim, uint32_t flags, float magnitude, void *stream) {
@@ -1368,12 +1436,12 @@ int srs_cache_write(srs_ctx *ctx, const srs_cache *cache, const srs_rows *k, con
     return launch_rope(a, cache->dtype, flags, st);
 }
 
+
 uint64_t srs_cache_attention_workspace(uint32_t nrequests, uint64_t tokens, uint32_t q_heads, uint32_t kv_heads, uint32_t head_dim,
                                        uint32_t table_width, uint32_t page_tokens, uint32_t window, uint32_t sinks,
                                        uint64_t most_tokens, uint64_t most_keys) {
-    (void)nrequests; (void)tokens; (void)q_heads; (void)kv_heads; (void)head_dim; (void)table_width; (void)page_tokens;
-    (void)window; (void)sinks; (void)most_tokens; (void)most_keys;
-    return 0;
+    if (nrequests == 0 || tokens == 0 || kv_heads == 0 || q_heads < kv_heads || tokens > kMaxIndexable || nrequests > kMaxIndexable) return 0;
+    return attention_plan(nrequests, tokens, q_heads, kv_heads, head_dim, table_width, page_tokens, window, sinks, most_tokens, most_keys).workspace;
 }
 
 int srs_cache_attention(srs_ctx *ctx, const srs_cache *cache, const srs_rows *q, const srs_rows *out, float *lse, uint64_t tokens,
@@ -1388,12 +1456,13 @@ int srs_cache_attention(srs_ctx *ctx, const srs_cache *cache, const srs_rows *q,
     if (tokens == 0 || nrequests == 0) return SRS_OK;
     if (!rows_ok(q, 16) || !rows_ok(out, 16) || q->heads != out->heads || q->heads % cache->heads) return SRS_ERR_INVALID;
     if (((q->token_stride | q->head_stride | out->token_stride | out->head_stride) & 7) != 0) return SRS_ERR_INVALID;
-    if (!token_begin || !start || (table_width && !table) || (uint64_t)table_width * cache->page_tokens > kMaxIndexable) return SRS_ERR_INVALID;
+    if (!token_begin || !start || (table_width && !table) || (uint64_t)table_width * cache->page_tokens > kMaxKeys) return SRS_ERR_INVALID;
     if (((uintptr_t)token_begin | (uintptr_t)start | (uintptr_t)table | (uintptr_t)lse) & 3u) return SRS_ERR_INVALID;
-    if (workspace_bytes < srs_cache_attention_workspace(nrequests, tokens, q->heads, cache->heads, cache->head_dim, table_width,
-                                                        cache->page_tokens, window, sinks, most_tokens, most_keys)) return SRS_ERR_INVALID;
-    (void)workspace;
-    if (tokens * q->heads > 0x7fffffffull) return SRS_ERR_INVALID;
+    const AttnPlan p = attention_plan(nrequests, tokens, q->heads, cache->heads, cache->head_dim, table_width, cache->page_tokens, window, sinks,
+                                      most_tokens, most_keys);
+    if (p.workspace && (!workspace || ((uintptr_t)workspace & 15u) || workspace_bytes < p.workspace)) return SRS_ERR_INVALID;
+    const uint64_t grid = (uint64_t)p.tiles * p.splits * cache->heads * p.head_blocks;
+    if (grid > 0x7fffffffull || tokens * q->heads > 0x7fffffffull) return SRS_ERR_INVALID;
     hipStream_t st = (hipStream_t)stream;
     SRS_ON_DEVICE(ctx->device);
     AttnArgs a;
@@ -1405,13 +1474,18 @@ int srs_cache_attention(srs_ctx *ctx, const srs_cache *cache, const srs_rows *q,
     a.v_page = cache->v_page; a.v_token = cache->v_token; a.v_head = cache->v_head;
     a.token_begin = token_begin; a.start = start; a.table = table;
     a.tokens = (uint32_t)tokens; a.nrequests = nrequests; a.width = table_width; a.page = cache->page_tokens; a.pages = cache->pages;
-    a.heads = q->heads; a.kv_heads = cache->heads; a.head_dim = cache->head_dim;
-    a.window = window; a.sinks = sinks; a.scale = scale; a.full = (flags & SRS_ATTN_FULL) != 0; a.flags = ctx->flags;
-    const dim3 grid((uint32_t)(tokens * q->heads));
-    if (cache->dtype == SRS_BF16) hipLaunchKernelGGL((attention_rows_kernel<__bf16>), grid, dim3(64), 0, st, a);
-    else hipLaunchKernelGGL((attention_rows_kernel<_Float16>), grid, dim3(64), 0, st, a);
-    SRS_HIP(hipGetLastError());
-    return SRS_OK;
+    a.page_shift = 32;
+    for (uint32_t k = 0; k < 31; ++k)
+        if (cache->page_tokens == 1u << k) a.page_shift = k;
+    a.heads = q->heads; a.kv_heads = cache->heads; a.head_dim = cache->head_dim; a.group = q->heads / cache->heads;
+    a.window = window; a.sinks = sinks; a.scale = scale * 1.44269504088896340736f; a.full = (flags & SRS_ATTN_FULL) != 0; a.flags = ctx->flags;
+    a.block = p.block; a.head_blocks = p.head_blocks; a.tile_tokens = p.tile_tokens; a.tiles = p.tiles;
+    a.splits = p.splits; a.split_tiles = p.split_tiles;
+    const uint64_t cells = tokens * q->heads;
+    a.part_o = (float *)workspace; a.part_lse = a.part_o + p.splits * cells * cache->head_dim; a.part_n = (uint32_t *)(a.part_lse + p.splits * cells);
+    const bool blocks = in_blocks(cache);
+    if (cache->dtype == SRS_BF16) return launch_attention<__bf16>(a, blocks, (uint32_t)grid, st);
+    return launch_attention<_Float16>(a, blocks, (uint32_t)grid, st);
 }
 
 // ---------------------------------------------------------------------------------------------

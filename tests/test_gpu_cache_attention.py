@@ -4,6 +4,8 @@ How far a result may be off: with A = sum_j p_j |v_j| over a row's normalised we
 * scores are binary32 sums of exact products: off by at most (D + 4) 2^-24 B, their weights by e^2 of that relatively, and exp adds 2^-22
   for itself and 2^-22 B for its argument in another base;
 * weights are rounded once to the element type: half a step h, relatively; that of the sum of weights cancels at best, so 2 h at worst;
+* weights below binary32's smallest normal number 2^-126 are 0 (the largest of a row is 1, so their sum is at least that): a value's part
+  of the result is then lost, |v_j| 2^-126 at most;
 * sums over n keys add n 2^-24, the joining of parts and the final division 2^-21;
 * the output is rounded once: h |o|.
 """
@@ -102,7 +104,7 @@ class Batch:
                 lse[rows, head] = torch.where(some, top[:, 0] + total[:, 0].log(), torch.full_like(top[:, 0], -math.inf))
                 B, n = size.amax(1), seen.sum(1)
                 score = (self.d + 4) * 2.0**-24 * B + 2.0**-22 * B + 2.0**-22
-                tol[rows, head] = h * o.abs() + A * (2 * h + 2 * score + n * 2.0**-24 + 2.0**-21)[:, None]
+                tol[rows, head] = h * o.abs() + A * (2 * h + 2 * score + n * 2.0**-24 + 2.0**-21)[:, None] + 2.0**-126 * vv[clean].abs().sum(0)
                 ltol[rows, head] = score + n * 2.0**-24 + 2.0**-21 + 2.0**-23 * lse[rows, head].abs().nan_to_num(0, 0, 0)
         return out, lse, tol, ltol
 
