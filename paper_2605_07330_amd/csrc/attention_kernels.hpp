@@ -4,9 +4,15 @@
 
 namespace srs {
 
-// The work: a tile is up to `rows` rows that share a key head, `block` heads of each of `tile_tokens` successive tokens of one
-// request.  Tiles are numbered so that a workgroup finds its own without a table: request r's begin at
-// token_begin[r] / tile_tokens + r, which leaves room for at least as many as it has.
+// How one of the two kernels lays its work out.  A tile is up to 16 (narrow) or 128 (wide) rows that share a key head: `block` heads of
+// each of `tile_tokens` successive tokens of one request.  Its keys may be shared out over `splits` workgroups, split_tiles key
+// tiles to each (the last takes what is left), whose results go to part_o [splits][slots][heads][head_dim] and part_lse [splits][slots][heads].
+struct AttnShape {
+    uint32_t block, head_blocks, tile_tokens, splits, split_tiles;
+    float *part_o, *part_lse;
+    uint64_t slots;
+};
+
 struct AttnArgs {
     const unsigned char *q, *k, *v;
     unsigned char *out;
@@ -14,16 +20,18 @@ struct AttnArgs {
     int64_t q_token, q_head, o_token, o_head;
     int64_t k_page, k_token, k_head, v_page, v_token, v_head;
     const int32_t *token_begin, *start, *table;
-    uint32_t tokens, nrequests, width, page, page_shift, pages;     // page_shift: log2 of page, or 32
+    uint32_t tokens, nrequests, width, page, pages;
+    uint32_t page_magic, page_shift;                                // j / page = j * page_magic >> page_shift for j below 2^31
     uint32_t heads, kv_heads, head_dim, group;
     uint32_t window, sinks;
-    float scale;                                                    // times log2(e)
+    float scale;                                                    // its size times log2(e); 1 where it is 0
+    float sign;                                                     // -1, 0 or 1: taken by the queries
     bool full;
     uint32_t *flags;
-    uint32_t block, head_blocks, tile_tokens, tiles;                // of this launch
-    uint32_t splits, split_tiles;                                   // parts of a request's keys, key tiles in each (the last: what is left)
-    float *part_o, *part_lse;                                       // [splits][tokens][heads][head_dim], [splits][tokens][heads]
-    uint32_t *part_n;                                               // [tokens][heads] parts that hold something
+    AttnShape narrow, wide;
+    uint32_t narrow_most;                                           // requests of more new tokens are the wide kernel's
+    uint32_t split_tokens;                                          // of more: not split by the narrow kernel
+    uint32_t wide_tiles;                                            // 0: there is no wide launch
 };
 
 template <class T> struct AttnTypes;
@@ -62,47 +70,90 @@ typedef const int32_t __attribute__((address_space(4))) const_i32;
 
 template <class T> __device__ __forceinline__ T uniform_value(T x) { return (T)__builtin_amdgcn_readfirstlane((int)x); }
 
+// Values that are not finite may not meet the weights of rows that do not see them (0 hides nothing), nor weights in two parts.  They are
+// taken out of the tile, and where there were any, what they add to the rows that do see them, themselves whatever their weights, is added
+// by a second walk over the keys when all else is done.
+template <class T> __device__ __forceinline__ u32x4 finite_values(u32x4 x) {
+    constexpr uint32_t E = AttnTypes<T>::kExponent;
+    u32x4 y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = x[e] & ((x[e] & E) == E ? 0xffff0000u : ~0u) & ((x[e] >> 16 & E) == E ? 0xffffu : ~0u);
+    return y;
+}
+
+// Queries take the scale's sign, so that the largest score is that of the largest product; 0 where there is none.
+template <class T> __device__ __forceinline__ typename AttnTypes<T>::x8 signed_query(typename AttnTypes<T>::x8 q, bool there, float sign) {
+    typename AttnTypes<T>::x8 y;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = (T)(there ? (float)q[e] * sign : 0.f);
+    return y;
+}
+
+// What the block table says about key j of a request, asked for early and looked at a key tile later, when the answer is there.
+// Nothing is asked where no row sees the key (or, with BLOCKS, any of the 16 keys that it is one of): place is then -1.
+struct Asked { int32_t page, place; };
+template <bool BLOCKS, class P>
+__device__ __forceinline__ Asked ask_table(const AttnArgs &a, P table, int32_t j, bool seen) {
+    const uint32_t at = (uint32_t)(((uint64_t)(uint32_t)j * a.page_magic) >> a.page_shift);
+    Asked x;
+    x.page = table[seen ? at : 0u];
+    x.place = seen ? j - (int32_t)(at * a.page) : -1;
+    return x;
+}
+
+// Bits 0 .. 63 of the keys from `key` on that a row sees: those before end, and at or after low or below sinks.
+__device__ __forceinline__ uint64_t bits_below(int32_t n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; }
+__device__ __forceinline__ uint64_t seen_bits(int32_t key, int32_t low, int32_t end, int32_t sinks) {
+    return bits_below(end - key) & (~bits_below(low - key) | bits_below(sinks - key));
+}
+
 struct AttnTile {
     int32_t r, first_row;              // request, row of its first token in the batch
-    int32_t i0, i1;                    // tokens of the tile, counted inside the request
+    int32_t i0, i1, n;                 // tokens of the tile, counted inside the request; of the request
     int64_t start;
     int32_t end;                       // keys that some row may see lie below
     int32_t low, sinks;                // and at or above low, or below sinks
     bool narrow;                       // the table ends before the keys do
 };
 
-// The request whose tiles hold number `tile`, by a search with 64 probes at a time; nothing where the tile is empty.
-__device__ __forceinline__ bool find_tile(const AttnArgs &a, uint32_t tile, AttnTile &t) {
-    const uint32_t lane = threadIdx.x & 63;
-    uint32_t lo = 0, hi = a.nrequests;
-    while (true) {
-        const uint32_t step = (hi - lo + 63) / 64, at = lo + lane * step;
-        bool before = false;
-        if (at < hi) {
-            const int32_t b = a.token_begin[at];
-            before = b >= 0 && (uint64_t)((uint32_t)b / a.tile_tokens) + at <= tile;
-        }
-        const uint32_t n = (uint32_t)__popcll(__ballot(before));
-        if (n == 0) return false;
-        lo += (n - 1) * step;
-        hi = lo + step < hi ? lo + step : hi;
-        if (step == 1) break;
-    }
-    lo = uniform_value(lo);
-    const int32_t b0 = a.token_begin[lo], b1 = a.token_begin[lo + 1], start = a.start[lo];
-    if (b0 < 0 || b1 < b0 || (uint32_t)b1 > a.tokens || start < 0) return false;
-    const int64_t i0 = (int64_t)(tile - ((uint32_t)b0 / a.tile_tokens + lo)) * a.tile_tokens;
-    if (i0 >= b1 - b0) return false;
-    t.r = (int32_t)lo; t.first_row = b0; t.start = start;
-    t.i0 = (int32_t)i0; t.i1 = b1 - b0 - t.i0 < (int32_t)a.tile_tokens ? b1 - b0 : t.i0 + (int32_t)a.tile_tokens;
-    const int64_t end = a.full ? (int64_t)start + (b1 - b0) : (int64_t)start + t.i1, room = (int64_t)a.width * a.page;
+// Request r, if it can be computed and has new tokens.
+__device__ __forceinline__ bool open_request(const AttnArgs &a, uint32_t r, AttnTile &t) {
+    const int32_t b0 = a.token_begin[r], b1 = a.token_begin[r + 1], start = a.start[r];
+    if (b0 < 0 || b1 <= b0 || (uint32_t)b1 > a.tokens || start < 0) return false;
+    t.r = (int32_t)r; t.first_row = b0; t.start = start; t.n = b1 - b0;
+    return true;
+}
+
+// Its tile that begins with token i0.
+__device__ __forceinline__ void open_tile(const AttnArgs &a, int32_t i0, uint32_t tile_tokens, AttnTile &t) {
+    t.i0 = i0; t.i1 = t.n - i0 < (int32_t)tile_tokens ? t.n : i0 + (int32_t)tile_tokens;
+    const int64_t end = t.start + (a.full ? t.n : t.i1), room = (int64_t)a.width * a.page;
     t.narrow = end > room;
     t.end = (int32_t)(end < room ? end : room);
-    int64_t low = a.window ? (int64_t)start + t.i0 - a.window + 1 : 0;
+    int64_t low = a.window ? t.start + t.i0 - a.window + 1 : 0;
     low = low < 0 ? 0 : low;
     t.low = (int32_t)(low < 0x7fffffff ? low : 0x7fffffff);
     t.sinks = a.window ? (int32_t)a.sinks : 0;
-    return true;
+}
+
+// The last request r with begin(r) <= at, begin(r) = token_begin[r] / tile_tokens + r * each, by a search with 64 probes at a time; -1
+// where there is none.
+__device__ __forceinline__ int32_t find_request(const AttnArgs &a, uint32_t at, uint32_t tile_tokens, uint32_t each) {
+    const uint32_t lane = threadIdx.x & 63;
+    uint32_t lo = 0, hi = a.nrequests;
+    while (true) {
+        const uint32_t step = (hi - lo + 63) / 64, r = lo + lane * step;
+        bool before = false;
+        if (r < hi) {
+            const int32_t b = a.token_begin[r];
+            before = b >= 0 && (uint64_t)((uint32_t)b / tile_tokens) + (uint64_t)r * each <= at;
+        }
+        const uint32_t n = (uint32_t)__popcll(__ballot(before));
+        if (n == 0) return -1;
+        lo += (n - 1) * step;
+        hi = lo + step < hi ? lo + step : hi;
+        if (step == 1) return uniform_value((int32_t)lo);
+    }
 }
 
 // The keys that a row at position pos sees: those before end, and at or after low or below the tile's sinks.
@@ -110,6 +161,20 @@ __device__ __forceinline__ void span(const AttnArgs &a, const AttnTile &t, int64
     end = a.full || pos + 1 >= t.end ? t.end : (int32_t)(pos + 1);
     const int64_t l = a.window ? pos - a.window + 1 : 0;
     low = l < 0 ? 0 : l < 0x7fffffff ? (int32_t)l : 0x7fffffff;
+}
+
+// add(row of V, whether this lane's row sees it) for the keys key .. key + n - 1 that some row sees
+template <class T, class F>
+__device__ __forceinline__ void walk_values(const AttnArgs &a, const AttnTile &t, uint32_t kh, int32_t key, int32_t n, int32_t row_low, int32_t row_end, F add) {
+    for (int32_t k = 0; k < n; ++k) {
+        const int32_t j = key + k;
+        if (j >= t.end || !(j >= t.low || j < t.sinks)) continue;
+        const uint32_t at = (uint32_t)(((uint64_t)(uint32_t)j * a.page_magic) >> a.page_shift);
+        const int32_t page = a.table[(int64_t)t.r * a.width + at];
+        if ((uint32_t)page >= a.pages) continue;
+        add((const T *)a.v + (int64_t)page * a.v_page + (int64_t)(j - (int32_t)(at * a.page)) * a.v_token + (int64_t)kh * a.v_head,
+            (j < row_end) & ((j >= row_low) | (j < t.sinks)));
+    }
 }
 
 // Requests that cannot be computed are reported by the launch's first workgroup.
@@ -135,25 +200,10 @@ struct KeyTiles {
     __device__ __forceinline__ int32_t key(int32_t i, int32_t step) const { return i < first ? i * step : low + (i - first) * step; }
 };
 
-// This part's share of them; the number of parts that have one.
-__device__ __forceinline__ uint32_t part_of(const AttnArgs &a, uint32_t split, int32_t all, int32_t &from, int32_t &to) {
-    uint32_t n = ((uint32_t)all + a.split_tiles - 1) / a.split_tiles;
-    n = n < 1 ? 1 : n > a.splits ? a.splits : n;
-    from = (int32_t)(split * a.split_tiles);
-    to = split + 1 == n ? all : from + (int32_t)a.split_tiles;
-    return n;
-}
-
-// o (normalised) and lse in base 2 of a row to where they belong.
-__device__ __forceinline__ void store_row_lse(const AttnArgs &a, uint64_t row, uint32_t head, uint32_t split, uint32_t n, float lse2) {
-    const uint64_t at = row * a.heads + head;
-    if (n > 1) {
-        a.part_lse[(uint64_t)split * a.tokens * a.heads + at] = lse2;
-        if (split == 0) a.part_n[at] = n;
-    } else {
-        if (a.splits > 1) a.part_n[at] = 1;
-        if (a.lse) a.lse[at] = lse2 * 0.69314718055994530942f;
-    }
+// How many parts the keys of a tile come in.
+__device__ __forceinline__ uint32_t parts_of(const AttnShape &w, int32_t all) {
+    const uint32_t n = ((uint32_t)all + w.split_tiles - 1) / w.split_tiles;
+    return n < 1 ? 1 : n > w.splits ? w.splits : n;
 }
 
 // ---- few rows: decoding ------------------------------------------------------------------------------------------------------
@@ -174,23 +224,29 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : DP == 128 ? 2 : 1) void attenti
     __shared__ __attribute__((aligned(16))) unsigned char s_mem[4 * kRegion];
     __shared__ float s_m[4][16], s_l[4][16];
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform_value(tid >> 6), g = lane >> 4, n = lane & 15;
+    const AttnShape &w = a.narrow;
     uint32_t id = blockIdx.x;
-    const uint32_t hb = id % (a.kv_heads * a.head_blocks), kh = hb / a.head_blocks, block = hb % a.head_blocks;
-    id /= a.kv_heads * a.head_blocks;
-    const uint32_t split = id % a.splits, tile = id / a.splits;
+    const uint32_t hb = id % (a.kv_heads * w.head_blocks), kh = hb / w.head_blocks, block = hb % w.head_blocks;
+    id /= a.kv_heads * w.head_blocks;
+    const uint32_t split = id % w.splits;
     if (blockIdx.x == 0) check_requests(a);
     AttnTile t;
-    if (!find_tile(a, tile, t)) return;
+    if (!open_request(a, id / w.splits, t) || (uint32_t)t.n > a.narrow_most) return;
+    // one tile, unless the caller's hint was wrong
+    for (int32_t i0 = 0; i0 < t.n; i0 += (int32_t)w.tile_tokens) {
+    if (i0) __syncthreads();
+    open_tile(a, i0, w.tile_tokens, t);
     const KeyTiles tiles(t, kNarrowKeys);
-    int32_t from, to;
-    const uint32_t parts = part_of(a, split, tiles.all, from, to);
+    const uint32_t parts = (uint32_t)t.n > a.split_tokens ? 1 : parts_of(w, tiles.all);
     if (split >= parts) return;
+    const int32_t from = (int32_t)(split * w.split_tiles);
+    int32_t to = split + 1 == parts ? tiles.all : from + (int32_t)w.split_tiles;
     if (a.pages == 0) to = from;
     bool bad = t.narrow || (a.pages == 0 && tiles.all > 0);
 
     // this lane's row: keys before row_end, and at or after row_low or before the sinks' end
-    const uint32_t token = n / a.block, head = block * a.block + n % a.block;
-    const bool row_ok = t.i0 + (int32_t)token < t.i1 && head < a.group && token < a.tile_tokens;
+    const uint32_t token = n / w.block, head = block * w.block + n % w.block;
+    const bool row_ok = t.i0 + (int32_t)token < t.i1 && head < a.group && token < w.tile_tokens;
     const uint64_t row = (uint64_t)(t.first_row + t.i0) + token;
     int32_t row_low, row_end, all_low, all_end;                                      // all: what every row of the tile sees
     span(a, t, t.start + t.i0 + token, row_low, row_end);
@@ -202,11 +258,11 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : DP == 128 ? 2 : 1) void attenti
 
     x8 q[kQC];
     {
-        const T *p = (const T *)a.q + (int64_t)row * a.q_token + (int64_t)(kh * a.group + head) * a.q_head;
+        const T *p = (const T *)a.q + (int64_t)(row_ok ? row : (uint64_t)(t.first_row + t.i0)) * a.q_token + (int64_t)(kh * a.group + (row_ok ? head : 0u)) * a.q_head;
 #pragma unroll
         for (int c = 0; c < kQC; ++c) {
-            x8 z = {};
-            q[c] = row_ok && (EXACT || c * 32 + g * 8 < a.head_dim) ? *(const x8 *)(p + c * 32 + g * 8) : z;
+            const bool there = EXACT || c * 32 + g * 8 < a.head_dim;
+            q[c] = signed_query<T>(*(const x8 *)(p + (there ? c * 32 + g * 8 : 0)), row_ok && there, a.sign);
         }
     }
 
@@ -218,47 +274,47 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : DP == 128 ? 2 : 1) void attenti
     const unsigned char *const k_base = a.k + (int64_t)kh * a.k_head * 2, *const v_base = a.v + (int64_t)kh * a.v_head * 2;
     const const_i32 *const table = (const const_i32 *)(a.table + (int64_t)t.r * a.width);
 
-    // What the table says for the 32 keys from `key` on: for both blocks of 16 where pages hold whole blocks (scalar loads), else for key +
-    // lane % 32.  Nothing is asked where no row sees a key; the answer is looked at a tile later, when it is there.
-    struct Asked { int32_t page[BLOCKS ? 2 : 1]; int32_t place[BLOCKS ? 2 : 1]; };
+    // pages of the 32 keys from `key` on: of both blocks of 16 where pages hold whole blocks (scalar), else of key + lane % 32
+    constexpr int kAsk = BLOCKS ? 2 : 1;
+    struct Questions { Asked x[kAsk]; };
     auto ask = [&](int32_t key, bool live) {
-        Asked w;
+        Questions x;
 #pragma unroll
-        for (int b = 0; b < (BLOCKS ? 2 : 1); ++b) {
+        for (int b = 0; b < kAsk; ++b) {
             const int32_t j = BLOCKS ? key + 16 * b : key + (int32_t)(lane & 31);
-            const uint32_t at = a.page_shift < 32 ? (uint32_t)j >> a.page_shift : (uint32_t)j / a.page;
-            const bool seen = live && j < t.end && (j + (BLOCKS ? 15 : 0) >= t.low || j < t.sinks);
-            w.page[b] = -1; w.place[b] = -1;
-            if (seen) {
-                w.page[b] = BLOCKS ? table[at] : a.table[(int64_t)t.r * a.width + at];
-                w.place[b] = j - (int32_t)(at * a.page);
-            }
+            const bool seen = live & (j < t.end) & ((j + (BLOCKS ? 15 : 0) >= t.low) | (j < t.sinks));
+            if constexpr (BLOCKS) x.x[b] = ask_table<true>(a, table, j, seen);
+            else x.x[b] = ask_table<false>(a, a.table + (int64_t)t.r * a.width, j, seen);
         }
-        return w;
+        return x;
     };
-    struct Pages { int32_t page[BLOCKS ? 2 : 1]; int32_t place[BLOCKS ? 2 : 1]; bool ok[BLOCKS ? 2 : 1]; };
-    auto take = [&](const Asked &w) {
+    struct Pages { int32_t page[kAsk], place[kAsk]; uint32_t ok; };                 // ok: bit k for key + k
+    auto take = [&](const Questions &x) {
         Pages p;
+        uint32_t ok = 0;
 #pragma unroll
-        for (int b = 0; b < (BLOCKS ? 2 : 1); ++b) {
-            p.ok[b] = (uint32_t)w.page[b] < a.pages;                                // -1 is not
-            bad |= w.place[b] >= 0 && !p.ok[b];
-            p.page[b] = p.ok[b] ? w.page[b] : 0;
-            p.place[b] = w.place[b] >= 0 ? w.place[b] : 0;
+        for (int b = 0; b < kAsk; ++b) {
+            const bool there = x.x[b].place >= 0 && (uint32_t)x.x[b].page < a.pages;
+            bad |= x.x[b].place >= 0 && !there;
+            p.page[b] = there ? x.x[b].page : 0;
+            p.place[b] = x.x[b].place >= 0 ? x.x[b].place : 0;
+            if constexpr (BLOCKS) ok |= there ? 0xffffu << (16 * b) : 0u;
+            else ok = (uint32_t)__ballot(there);
         }
+        p.ok = ok;
         return p;
     };
     x8 kreg[2][kQC];
     u32x4 vreg[kVC];
-    auto load_k = [&](const Pages &w) {
+    auto load_k = [&](const Pages &pg) {
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             gptr<const unsigned char> p;
             uint32_t off = k_lane;
             if constexpr (BLOCKS) {
-                p = scalar_base(as_global(k_base + ((int64_t)w.page[b] * a.k_page + (int64_t)w.place[b] * a.k_token) * 2));
+                p = scalar_base(as_global(k_base + ((int64_t)pg.page[b] * a.k_page + (int64_t)pg.place[b] * a.k_token) * 2));
             } else {
-                p = as_global(k_base + ((int64_t)__shfl(w.page[0], 16 * b + n) * a.k_page + (int64_t)__shfl(w.place[0], 16 * b + n) * a.k_token) * 2);
+                p = as_global(k_base + ((int64_t)__shfl(pg.page[0], 16 * b + n) * a.k_page + (int64_t)__shfl(pg.place[0], 16 * b + n) * a.k_token) * 2);
                 off = g * 16;
             }
 #pragma unroll
@@ -274,65 +330,61 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : DP == 128 ? 2 : 1) void attenti
             }
         }
     };
-    auto load_v = [&](const Pages &w) {
+    auto load_v = [&](const Pages &pg) {
 #pragma unroll
         for (int c = 0; c < kVC; ++c) {
             constexpr int kLoads = 16 / kRowsPerLoad;                               // of a block
             if constexpr (BLOCKS) {
                 const int b = c / kLoads;
-                const auto p = scalar_base(as_global(v_base + ((int64_t)w.page[b] * a.v_page + ((int64_t)w.place[b] + (c % kLoads) * kRowsPerLoad) * a.v_token) * 2));
+                const auto p = scalar_base(as_global(v_base + ((int64_t)pg.page[b] * a.v_page + ((int64_t)pg.place[b] + (c % kLoads) * kRowsPerLoad) * a.v_token) * 2));
                 vreg[c] = *(gptr<const u32x4>)(p + v_lane);
             } else {
                 const uint32_t k = c * kRowsPerLoad + vrow;
-                const auto p = as_global(v_base + ((int64_t)__shfl(w.page[0], k) * a.v_page + (int64_t)__shfl(w.place[0], k) * a.v_token) * 2);
+                const auto p = as_global(v_base + ((int64_t)__shfl(pg.page[0], k) * a.v_page + (int64_t)__shfl(pg.place[0], k) * a.v_token) * 2);
                 vreg[c] = *(gptr<const u32x4>)(p + (v_lane - vrow * (uint32_t)a.v_token * 2));
             }
         }
     };
     unsigned char *const mine = s_mem + wave * kRegion;
     auto place_of = [&](uint32_t key, uint32_t piece) { return key * (DP * 2) + ((piece ^ ((key & 7) << 1)) & (kRowPieces - 1)) * 16; };
-    auto visible = [&](const Pages &w, int32_t key, uint32_t k) {                   // key + k to this lane's row
-        const int32_t j = key + (int32_t)k;
-        const bool ok = BLOCKS ? (k < 16 ? w.ok[0] : w.ok[BLOCKS ? 1 : 0]) : __shfl((int)w.ok[0], (int)k) != 0;
-        return ok & (j < row_end) & ((j >= row_low) | (j < t.sinks));
-    };
-
     f32x4 o[kVC];
 #pragma unroll
     for (int c = 0; c < kVC; ++c) o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
+    bool dirty = false;
     const int32_t shift = 32 * (int32_t)wave;
+    if (from < to) {
     Pages now = take(ask(tiles.key(from, kNarrowKeys) + shift, from < to));
-    Asked next = ask(tiles.key(from + 1, kNarrowKeys) + shift, from + 1 < to);
-    if (from < to) { load_v(now); load_k(now); }
+    Questions next = ask(tiles.key(from + 1, kNarrowKeys) + shift, from + 1 < to);
+    load_v(now); load_k(now);
 #pragma unroll 1
     for (int32_t i = from; i < to; ++i) {
         const int32_t key = tiles.key(i, kNarrowKeys) + shift;
         const bool more = i + 1 < to;
         // does every row see every one of these keys?
-        const bool whole = key + 32 <= all_end && (key >= all_low || key + 32 <= t.sinks) && (BLOCKS ? now.ok[0] && now.ok[BLOCKS ? 1 : 0] : (bool)__all(now.ok[0]));
+        const bool whole = key + 32 <= all_end && (key >= all_low || key + 32 <= t.sinks) && now.ok == ~0u;
         if (!whole) {
             // values that no row sees are 0: a weight of 0 does not hide what is not a number
+            const uint32_t any = (uint32_t)seen_bits(key, t.low, t.end, t.sinks) & now.ok;
 #pragma unroll
             for (int c = 0; c < kVC; ++c) {
-                const uint32_t k = c * kRowsPerLoad + vrow;
-                const int32_t j = key + (int32_t)k;
-                const bool ok = BLOCKS ? now.ok[BLOCKS ? (c * kRowsPerLoad) >> 4 : 0] : __shfl((int)now.ok[0], (int)k) != 0;
-                const bool any = ok & (j < t.end) & ((j >= t.low) | (j < t.sinks));
-                vreg[c] = u32x4{any ? vreg[c][0] : 0u, any ? vreg[c][1] : 0u, any ? vreg[c][2] : 0u, any ? vreg[c][3] : 0u};
+                const bool here = any >> (c * kRowsPerLoad + vrow) & 1u;
+                vreg[c] = u32x4{here ? vreg[c][0] : 0u, here ? vreg[c][1] : 0u, here ? vreg[c][2] : 0u, here ? vreg[c][3] : 0u};
             }
         }
-        // values that are not finite are left out of the product and added row by row, for the rows that see them: the product would
-        // take them times the weights of the others, and times both parts of a weight
         u16x2 largest = {0, 0};
 #pragma unroll
         for (int c = 0; c < kVC; ++c)
 #pragma unroll
             for (int e = 0; e < 4; ++e) largest = __builtin_elementwise_max(largest, __builtin_bit_cast(u16x2, vreg[c][e] & 0x7fff7fffu));
-        const bool dirty = __any((largest[0] >= AttnTypes<T>::kExponent) | (largest[1] >= AttnTypes<T>::kExponent));
+        if (__any((largest[0] >= AttnTypes<T>::kExponent) | (largest[1] >= AttnTypes<T>::kExponent))) {
+            dirty = true;
+#pragma unroll
+            for (int c = 0; c < kVC; ++c) vreg[c] = finite_values<T>(vreg[c]);
+        }
 #pragma unroll
         for (int c = 0; c < kVC; ++c) *(u32x4 *)(mine + place_of(c * kRowsPerLoad + vrow, vpiece)) = vreg[c];
-        const Pages cur = now;
+        const uint32_t ok = now.ok;
         now = take(next);
         next = ask(tiles.key(i + 2, kNarrowKeys) + shift, i + 2 < to);
         if (more) load_v(now);
@@ -347,8 +399,9 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : DP == 128 ? 2 : 1) void attenti
         }
         if (more) load_k(now);
         if (!whole) {
+            const uint32_t sees = ((uint32_t)seen_bits(key, row_low, row_end, t.sinks) & ok) >> (4 * g);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = visible(cur, key, 16 * (e >> 2) + 4 * g + (e & 3)) ? x[e] : -INFINITY;
+            for (int e = 0; e < 8; ++e) x[e] = sees >> (16 * (e >> 2) + (e & 3)) & 1u ? x[e] : -INFINITY;
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) top = fmaxf(top, x[e]);
@@ -370,44 +423,26 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : DP == 128 ? 2 : 1) void attenti
             high[e] = (T)x[e];
             rest[e] = (T)(x[e] - (float)high[e]);
         }
-        if (dirty) {
-            // weights times values that are not finite, for the rows that see them; then the values are 0
-#pragma unroll 1
-            for (uint32_t k = 0; k < 32; ++k) {
-                float w = x[0];
-#pragma unroll
-                for (int e = 1; e < 8; ++e) w = (k >> 4) * 4 + (k & 3) == (uint32_t)e ? x[e] : w;
-                w = __shfl(w, (int)((k >> 2 & 3) * 16 + n));
-                const bool sees = visible(cur, key, k);
-#pragma unroll
-                for (int c = 0; c < kVC; ++c) {
-                    const T *const at = (const T *)(mine + place_of(k, 2 * c + (g >> 1)) + (g & 1) * 8);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float v = (float)at[e];
-                        o[c][e] += (sees && !(fabsf(v) < INFINITY)) ? w * v : 0.f;
-                    }
-                }
-            }
-#pragma unroll 1
-            for (uint32_t c = 0; c < (uint32_t)kVC; ++c) {
-                uint32_t *const at = (uint32_t *)(mine + place_of(c * kRowsPerLoad + vrow, vpiece));
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t E = AttnTypes<T>::kExponent, y = at[e];
-                    at[e] = y & ((y & E) == E ? 0xffff0000u : ~0u) & ((y >> 16 & E) == E ? 0xffffu : ~0u);
-                }
-            }
-        }
+        auto values = [&](int c, int b) { return lds_transposed(mine + place_of(16 * b + 4 * g + (n >> 2), 2 * c + ((n & 3) >> 1)) + (n & 1) * 8); };
 #pragma unroll
         for (int c = 0; c < kVC; ++c) {
-            s16x4 v[2];
-#pragma unroll
-            for (int b = 0; b < 2; ++b) v[b] = lds_transposed(mine + place_of(16 * b + 4 * g + (n >> 2), 2 * c + ((n & 3) >> 1)) + (n & 1) * 8);
-            const x8 vt = __builtin_bit_cast(x8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
+            const x8 vt = __builtin_bit_cast(x8, __builtin_shufflevector(values(c, 0), values(c, 1), 0, 1, 2, 3, 4, 5, 6, 7));
             o[c] = mfma_16x16x32(vt, high, o[c]);
             o[c] = mfma_16x16x32(vt, rest, o[c]);
         }
+    }
+    if (dirty) {
+        for (int32_t i = from; i < to; ++i)
+            walk_values<T>(a, t, kh, tiles.key(i, kNarrowKeys) + shift, 32, row_low, row_end, [&](const T *v, bool sees) {
+#pragma unroll
+                for (int c = 0; c < kVC; ++c)
+                    if (EXACT || c * 16 + g * 4 < a.head_dim) {
+                        const x4 y = *(const x4 *)(v + c * 16 + g * 4);
+                        o[c] += f32x4{sees && !(fabsf((float)y[0]) < INFINITY) ? (float)y[0] : 0.f, sees && !(fabsf((float)y[1]) < INFINITY) ? (float)y[1] : 0.f,
+                                      sees && !(fabsf((float)y[2]) < INFINITY) ? (float)y[2] : 0.f, sees && !(fabsf((float)y[3]) < INFINITY) ? (float)y[3] : 0.f};
+                    }
+            });
+    }
     }
     if (bad) atomicOr(a.flags, kFlagBadIndex);
 
@@ -419,18 +454,19 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : DP == 128 ? 2 : 1) void attenti
     for (int c = 0; c < kVC; ++c) *(f32x4 *)(os + n * (DP + 4) + c * 16 + g * 4) = o[c];
     if (lane < 16) { s_m[wave][lane] = m; s_l[wave][lane] = l; }
     __syncthreads();
-    const uint32_t orow = tid >> 4, otoken = orow / a.block, ohead = block * a.block + orow % a.block;
-    if (t.i0 + (int32_t)otoken >= t.i1 || ohead >= a.group || otoken >= a.tile_tokens) return;
-    float M = -INFINITY, L = 0.f, w[4];
+    const uint32_t orow = tid >> 4, otoken = orow / w.block, ohead = block * w.block + orow % w.block;
+    if (t.i0 + (int32_t)otoken >= t.i1 || ohead >= a.group || otoken >= w.tile_tokens) continue;
+    float M = -INFINITY, L = 0.f, share[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) M = fmaxf(M, s_m[k][orow]);
     const float base = M == -INFINITY ? 0.f : M;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) { w[k] = __builtin_amdgcn_exp2f(s_m[k][orow] - base); L += w[k] * s_l[k][orow]; }
+    for (int k = 0; k < 4; ++k) { share[k] = __builtin_amdgcn_exp2f(s_m[k][orow] - base); L += share[k] * s_l[k][orow]; }
     const bool some = !(M == -INFINITY && L == 0.f);
     const float inv = some ? 1.f / L : 0.f;
     const uint64_t out_row = (uint64_t)(t.first_row + t.i0) + otoken;
     const uint32_t out_head = kh * a.group + ohead;
+    const uint64_t cell = (split * w.slots + (uint64_t)t.r * a.split_tokens + otoken) * a.heads + out_head;     // where parts > 1
 #pragma unroll
     for (int c = 0; c < DP / 64; ++c) {
         const uint32_t d = c * 64 + (tid & 15) * 4;
@@ -440,64 +476,372 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : DP == 128 ? 2 : 1) void attenti
         for (int k = 0; k < 4; ++k) {
             const f32x4 part = *(const f32x4 *)((const float *)(s_mem + k * kRegion) + orow * (DP + 4) + d);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] += w[k] * part[e];
+            for (int e = 0; e < 4; ++e) y[e] += share[k] * part[e];
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) y[e] = some ? y[e] * inv : 0.f;
         if (parts > 1) {
-            *(f32x4 *)(a.part_o + (((uint64_t)split * a.tokens + out_row) * a.heads + out_head) * a.head_dim + d) = f32x4{y[0], y[1], y[2], y[3]};
+            *(f32x4 *)(w.part_o + cell * a.head_dim + d) = f32x4{y[0], y[1], y[2], y[3]};
         } else {
             *(x4 *)((T *)a.out + (int64_t)out_row * a.o_token + (int64_t)out_head * a.o_head + d) = x4{(T)y[0], (T)y[1], (T)y[2], (T)y[3]};
         }
     }
-    if ((tid & 15) == 0) store_row_lse(a, out_row, out_head, split, parts, some ? base + __builtin_amdgcn_logf(L) - AttnTypes<T>::kShift : -INFINITY);
+    if ((tid & 15) == 0) {
+        const float lse2 = some ? base + __builtin_amdgcn_logf(L) - AttnTypes<T>::kShift : -INFINITY;
+        if (parts > 1) w.part_lse[cell] = lse2;
+        else if (a.lse) a.lse[out_row * a.heads + out_head] = lse2 * 0.69314718055994530942f;
+    }
+    }
+}
+
+// ---- many rows: chunks ---------------------------------------------------------------------------------------------------------
+// 128 rows to a workgroup, 32 to each of its four waves, which all go through the tile's keys, 64 at a time.  K and V of a key tile pass
+// through LDS (two buffers; the next tile is on its way in registers meanwhile), where every wave takes them as the left operand of
+// v_mfma 32x32x16: S^T = K Q^T, so that a lane holds the weights of one row, and O^T = V^T P^T with P^T straight from those registers, the
+// keys of a product counted in the order in which the lanes have them.  Pieces of 16 bytes are rearranged in each row so that neither
+// the rows of K nor the transposed reads of V meet on a bank.  Weights are rounded to the element type for the second product.  A row's
+// accumulators follow its running maximum only when that has grown by 2^kSlack.
+// Bound: the matrix units, then LDS reads and the exponentials beside them.
+constexpr float kSlack = 8.f;
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+__device__ __forceinline__ f32x16 mfma_32x32x16(AttnTypes<__bf16>::x8 a, AttnTypes<__bf16>::x8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mfma_32x32x16(AttnTypes<_Float16>::x8 a, AttnTypes<_Float16>::x8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+
+template <class T, int DP, bool BLOCKS, bool EXACT>
+__global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_wide_kernel(const AttnArgs a) {
+    typedef typename AttnTypes<T>::x8 x8;
+    typedef typename AttnTypes<T>::x4 x4;
+    constexpr int KT = DP <= 128 ? 64 : 32, kB = KT / 32, kQC = DP / 16, kDB = DP / 32, kRowPieces = DP / 8;
+    constexpr int kRowsPerLoad = 256 / kRowPieces, kRowsPerWave = kRowsPerLoad / 4, kLoads = KT / kRowsPerLoad, kBytes = KT * DP * 2;
+    constexpr float kShift = AttnTypes<T>::kShift == 0.f ? 0.f : 6.f;              // with kSlack: at most 2^14 in a half
+    __shared__ __attribute__((aligned(16))) unsigned char s_k[2][kBytes], s_v[2][kBytes];
+    __shared__ unsigned char s_ok[2][KT];                                          // is the key's page there
+    __shared__ int32_t s_holes[2], s_dirty;                                        // the last tile in the buffer with a key that is not; was a value not finite
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform_value(tid >> 6), h = lane >> 5, n = lane & 31;
+    const AttnShape &w = a.wide;
+    uint32_t id = blockIdx.x;
+    const uint32_t hb = id % (a.kv_heads * w.head_blocks), kh = hb / w.head_blocks, block = hb % w.head_blocks;
+    id /= a.kv_heads * w.head_blocks;
+    const uint32_t split = id % w.splits, tile = a.wide_tiles - 1 - id / w.splits;  // later tokens, which see more keys, first
+    AttnTile t;
+    const int32_t r = find_request(a, tile, w.tile_tokens, 1);
+    if (r < 0 || !open_request(a, (uint32_t)r, t) || (uint32_t)t.n <= a.narrow_most) return;
+    const int64_t i0 = (int64_t)(tile - ((uint32_t)t.first_row / w.tile_tokens + (uint32_t)r)) * w.tile_tokens;
+    if (i0 >= t.n) return;
+    open_tile(a, (int32_t)i0, w.tile_tokens, t);
+    const KeyTiles tiles(t, KT);
+    const uint32_t parts = parts_of(w, tiles.all);
+    if (split >= parts) return;
+    const int32_t from = (int32_t)(split * w.split_tiles);
+    int32_t to = split + 1 == parts ? tiles.all : from + (int32_t)w.split_tiles;
+    if (a.pages == 0) to = from;
+    bool bad = t.narrow || (a.pages == 0 && tiles.all > 0);
+
+    // this lane's row, and what some and all rows of the wave see
+    const uint32_t slot = wave * 32 + n, token = slot / w.block, head = block * w.block + slot % w.block;
+    const bool row_ok = t.i0 + (int32_t)token < t.i1 && head < a.group && token < w.tile_tokens;
+    const uint64_t row = (uint64_t)(t.first_row + t.i0) + token;
+    const int32_t tokens = t.i1 - t.i0, first = (int32_t)(wave * 32 / w.block), last_full = (int32_t)((wave * 32 + 31) / w.block);
+    const int32_t last = last_full < tokens ? last_full : tokens - 1;
+    int32_t row_low, row_end, all_low, all_end, any_low, any_end;
+    span(a, t, t.start + t.i0 + token, row_low, row_end);
+    span(a, t, t.start + t.i0 + first, any_low, all_end);
+    span(a, t, t.start + t.i0 + last, all_low, any_end);
+    if (first >= tokens) any_end = 0;                                              // no row at all
+
+    x8 q[kQC];
+    {
+        const T *p = (const T *)a.q + (int64_t)(row_ok ? row : (uint64_t)(t.first_row + t.i0)) * a.q_token + (int64_t)(kh * a.group + (row_ok ? head : 0u)) * a.q_head;
+#pragma unroll
+        for (int c = 0; c < kQC; ++c) {
+            const bool there = EXACT || c * 16 + h * 8 < a.head_dim;
+            q[c] = signed_query<T>(*(const x8 *)(p + (there ? c * 16 + h * 8 : 0)), row_ok && there, a.sign);
+        }
+    }
+
+    // A thread carries piece `piece` of row c * kRowsPerLoad + my_row of every key tile, of K and of V.
+    const uint32_t piece = lane % kRowPieces, lane_row = lane / kRowPieces, my_row = wave * kRowsPerWave + lane_row;
+    const bool inside = EXACT || piece * 8 < a.head_dim;
+    const uint32_t piece_off = inside ? piece * 16 : 0;
+    const uint32_t k_lane = lane_row * (uint32_t)a.k_token * 2 + piece_off, v_lane = lane_row * (uint32_t)a.v_token * 2 + piece_off;
+    const unsigned char *const k_base = a.k + (int64_t)kh * a.k_head * 2, *const v_base = a.v + (int64_t)kh * a.v_head * 2;
+    const const_i32 *const table = (const const_i32 *)(a.table + (int64_t)t.r * a.width);
+    struct Questions { Asked x[kLoads]; };
+    auto ask = [&](int32_t key, bool live) {
+        Questions x;
+#pragma unroll
+        for (int c = 0; c < kLoads; ++c) {
+            const int32_t j = key + c * kRowsPerLoad + (int32_t)(BLOCKS ? wave * kRowsPerWave : my_row), b = BLOCKS ? j & ~15 : j;
+            const bool seen = live & (b < t.end) & ((b + (BLOCKS ? 15 : 0) >= t.low) | (b < t.sinks));
+            if constexpr (BLOCKS) x.x[c] = ask_table<true>(a, table, j, seen);
+            else x.x[c] = ask_table<false>(a, a.table + (int64_t)t.r * a.width, j, seen);
+        }
+        return x;
+    };
+    u32x4 kst[kLoads], vst[kLoads];
+    uint32_t ok = 0;                                                               // bit c: the row that load c brought is there
+    bool hole = false;
+    auto load = [&](const Questions &x) {
+        hole = false; ok = 0;
+#pragma unroll
+        for (int c = 0; c < kLoads; ++c) {
+            const bool there = x.x[c].place >= 0 && (uint32_t)x.x[c].page < a.pages;
+            hole |= x.x[c].place >= 0 && !there;
+            ok |= there ? 1u << c : 0u;
+            const int64_t page = there ? x.x[c].page : 0, place = x.x[c].place >= 0 ? x.x[c].place : 0;
+            if constexpr (BLOCKS) {
+                kst[c] = *(gptr<const u32x4>)(scalar_base(as_global(k_base + (page * a.k_page + place * a.k_token) * 2)) + k_lane);
+                vst[c] = *(gptr<const u32x4>)(scalar_base(as_global(v_base + (page * a.v_page + place * a.v_token) * 2)) + v_lane);
+            } else {
+                kst[c] = *(gptr<const u32x4>)as_global(k_base + (page * a.k_page + place * a.k_token) * 2 + piece_off);
+                vst[c] = *(gptr<const u32x4>)as_global(v_base + (page * a.v_page + place * a.v_token) * 2 + piece_off);
+            }
+            if constexpr (!EXACT) kst[c] = u32x4{inside ? kst[c][0] : 0u, inside ? kst[c][1] : 0u, inside ? kst[c][2] : 0u, inside ? kst[c][3] : 0u};
+        }
+        bad |= hole;
+    };
+    auto k_place = [&](uint32_t key, uint32_t p) { return key * (DP * 2) + (p ^ (DP == 64 ? (key >> 1) & 7 : key & 15)) * 16; };
+    auto v_place = [&](uint32_t key, uint32_t p) { return key * (DP * 2) + (p ^ (DP == 64 ? ((key >> 1) & 1) << 2 : (key & 3) << 2)) * 16; };
+    int32_t whole_low, whole_end, unused;                                          // what every row of the tile sees
+    span(a, t, t.start + t.i1 - 1, whole_low, unused);
+    span(a, t, t.start + t.i0, unused, whole_end);
+    // what the registers hold, tile i with keys from `key` on, into LDS
+    auto put = [&](int32_t i, int32_t key) {
+        const int buf = i & 1;
+        const bool edge = !(key + KT <= t.end && (key >= t.low || key + KT <= t.sinks));
+        const bool holes = __any(hole);
+        u16x2 largest = {0, 0};
+        if (edge || holes) {                                                      // values that no row sees are 0
+            const uint64_t any = seen_bits(key, t.low, t.end, t.sinks) >> my_row;
+#pragma unroll
+            for (int c = 0; c < kLoads; ++c) {
+                const bool here = (any >> (c * kRowsPerLoad) & 1u) & (ok >> c & 1u);
+                vst[c] = u32x4{here ? vst[c][0] : 0u, here ? vst[c][1] : 0u, here ? vst[c][2] : 0u, here ? vst[c][3] : 0u};
+            }
+        }
+        // where some row does not see every key it matters whether a value is finite
+        if (!(key + KT <= whole_end && (key >= whole_low || key + KT <= t.sinks))) {
+#pragma unroll
+            for (int c = 0; c < kLoads; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) largest = __builtin_elementwise_max(largest, __builtin_bit_cast(u16x2, vst[c][e] & 0x7fff7fffu));
+            if (__any((largest[0] >= AttnTypes<T>::kExponent) | (largest[1] >= AttnTypes<T>::kExponent))) {
+                if (lane == 0) s_dirty = 1;
+#pragma unroll
+                for (int c = 0; c < kLoads; ++c) vst[c] = finite_values<T>(vst[c]);
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < kLoads; ++c) {
+            const uint32_t row = c * kRowsPerLoad + my_row;
+            *(u32x4 *)(s_k[buf] + k_place(row, piece)) = kst[c];
+            *(u32x4 *)(s_v[buf] + v_place(row, piece)) = vst[c];
+        }
+        if (piece == 0) {
+#pragma unroll
+            for (int c = 0; c < kLoads; ++c) s_ok[buf][c * kRowsPerLoad + my_row] = (unsigned char)(ok >> c & 1u);
+        }
+        if (holes && lane == 0) s_holes[buf] = i;
+    };
+
+    f32x16 o[kDB];
+#pragma unroll
+    for (int d = 0; d < kDB; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
+    float m = -INFINITY, l = 0.f;
+    if (tid < 2) { s_holes[tid] = -1; s_dirty = 0; }
+    __syncthreads();
+    if (from < to) {
+    Questions next = ask(tiles.key(from, KT), true);
+    {
+        load(next);
+        next = ask(tiles.key(from + 1, KT), from + 1 < to);
+        put(from, tiles.key(from, KT));
+    }
+    __syncthreads();
+
+#pragma unroll 1
+    for (int32_t i = from; i < to; ++i) {
+        const int buf = i & 1;
+        const int32_t key = tiles.key(i, KT);
+        const bool more = i + 1 < to;
+        if (more) load(next);
+        next = ask(tiles.key(i + 2, KT), i + 2 < to);
+        if (key < any_end && (key + KT > any_low || key < t.sinks)) {              // some row of the wave sees something
+            const bool holes = uniform_value(s_holes[buf]) == i;
+            const bool whole = key + KT <= all_end && (key >= all_low || key + KT <= t.sinks) && !holes;
+            float x[kB][16], top = -INFINITY;
+#pragma unroll
+            for (int b = 0; b < kB; ++b) {
+                f32x16 s;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[e] = 0.f;
+#pragma unroll
+                for (int c = 0; c < kQC; ++c) s = mfma_32x32x16(*(const x8 *)(s_k[buf] + k_place(32 * b + n, 2 * c + h)), q[c], s);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) x[b][e] = s[e];
+            }
+            if (!whole) {
+                uint64_t sees = seen_bits(key, row_low, row_end, t.sinks);
+                if (holes) sees &= __ballot(s_ok[buf][lane % KT] != 0);
+                const uint64_t mine = sees >> (4 * h);
+#pragma unroll
+                for (int b = 0; b < kB; ++b)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) x[b][e] = (uint32_t)(mine >> (32 * b)) >> (8 * (e / 4) + e % 4) & 1u ? x[b][e] : -INFINITY;
+            }
+#pragma unroll
+            for (int b = 0; b < kB; ++b)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) top = fmaxf(top, x[b][e]);
+            top = fmaxf(top, __shfl_xor(top, 32)) * a.scale;
+            if (__any(top > m + kSlack)) {
+                const float m2 = fmaxf(m, top), keep = m2 == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m2);
+                l *= keep;
+#pragma unroll
+                for (int d = 0; d < kDB; ++d) o[d] *= keep;
+                m = m2;
+            }
+            const float base = kShift - (m == -INFINITY ? 0.f : m);
+            x8 p[kB][2];
+#pragma unroll
+            for (int b = 0; b < kB; ++b)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    x[b][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][e], a.scale, base));
+                    l += x[b][e];
+                    p[b][e / 8][e % 8] = (T)x[b][e];
+                }
+            auto values = [&](int d, int b, int c, int u) {
+                return lds_transposed(s_v[buf] + v_place(32 * b + 16 * c + 8 * u + 4 * h + ((lane & 15) >> 2), 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + (lane & 1) * 8);
+            };
+#pragma unroll
+            for (int b = 0; b < kB; ++b)
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int d = 0; d < kDB; ++d)
+                        o[d] = mfma_32x32x16(__builtin_bit_cast(x8, __builtin_shufflevector(values(d, b, c, 0), values(d, b, c, 1), 0, 1, 2, 3, 4, 5, 6, 7)), p[b][c], o[d]);
+        }
+        if (more) put(i + 1, tiles.key(i + 1, KT));
+        __syncthreads();
+    }
+    if (uniform_value(s_dirty)) {
+        for (int32_t i = from; i < to; ++i)
+            walk_values<T>(a, t, kh, tiles.key(i, KT), KT, row_low, row_end, [&](const T *v, bool sees) {
+#pragma unroll
+                for (int d = 0; d < kDB; ++d)
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+                        if (EXACT || 32 * d + 8 * u + 4 * h < a.head_dim) {
+                            const x4 y = *(const x4 *)(v + 32 * d + 8 * u + 4 * h);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) o[d][4 * u + e] += sees && !(fabsf((float)y[e]) < INFINITY) ? (float)y[e] : 0.f;
+                        }
+            });
+    }
+    }
+    if (bad) atomicOr(a.flags, kFlagBadIndex);
+
+    l += __shfl_xor(l, 32);
+    if (!row_ok) return;
+    const bool some = !(m == -INFINITY && l == 0.f);
+    const float inv = some ? 1.f / l : 0.f;
+    const uint32_t out_head = kh * a.group + head;
+    const uint64_t cell = (split * w.slots + row) * a.heads + out_head;                         // where parts > 1
+    auto each = [&](auto store) {
+#pragma unroll
+        for (int d = 0; d < kDB; ++d)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const uint32_t at = 32 * d + 8 * u + 4 * h;
+                if (EXACT || at < a.head_dim)
+                    store(at, some ? o[d][4 * u] * inv : 0.f, some ? o[d][4 * u + 1] * inv : 0.f, some ? o[d][4 * u + 2] * inv : 0.f, some ? o[d][4 * u + 3] * inv : 0.f);
+            }
+    };
+    if (parts > 1) {
+        float *const to_p = w.part_o + cell * a.head_dim;
+        each([&](uint32_t at, float y0, float y1, float y2, float y3) { *(f32x4 *)(to_p + at) = f32x4{y0, y1, y2, y3}; });
+    } else {
+        T *const to_p = (T *)a.out + (int64_t)row * a.o_token + (int64_t)out_head * a.o_head;
+        each([&](uint32_t at, float y0, float y1, float y2, float y3) { *(x4 *)(to_p + at) = x4{(T)y0, (T)y1, (T)y2, (T)y3}; });
+    }
+    if (h == 0) {
+        const float lse2 = some ? m + __builtin_amdgcn_logf(l) - kShift : -INFINITY;
+        if (parts > 1) w.part_lse[cell] = lse2;
+        else if (a.lse) a.lse[row * a.heads + out_head] = lse2 * 0.69314718055994530942f;
+    }
 }
 
 // ---- joining the parts -------------------------------------------------------------------------------------------------------
-// A wave per row and head whose keys were shared out: parts' results weighted by exp2 of their lse.
-template <class T>
+// A workgroup per row and head whose keys were shared out: the parts' results weighted by exp2 of their lse.  Eight parts are read at
+// once (32 threads take four elements each of one, four parts in flight each), so that hundreds of parts cost a few round trips.
+template <class T, bool WIDE>
 __global__ __launch_bounds__(256) void attention_join_kernel(const AttnArgs a) {
-    const uint32_t lane = threadIdx.x & 63;
-    const uint64_t at = (uint64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (at >= (uint64_t)a.tokens * a.heads) return;
-    const uint32_t row = (uint32_t)(at / a.heads), head = (uint32_t)(at % a.heads);
-    // is the row one of a request that was computed?
-    uint32_t lo = 0, hi = a.nrequests;
-    while (true) {
-        const uint32_t step = (hi - lo + 63) / 64, k = lo + lane * step;
-        const bool before = k < hi && a.token_begin[k] >= 0 && a.token_begin[k] <= (int32_t)row;
-        const uint32_t n = (uint32_t)__popcll(__ballot(before));
-        if (n == 0) return;
-        lo += (n - 1) * step;
-        hi = lo + step < hi ? lo + step : hi;
-        if (step == 1) break;
+    __shared__ float s_top[4], s_sum[8];
+    __shared__ f32x4 s_o[8][64];
+    const uint32_t tid = threadIdx.x, lane = tid & 63;
+    const AttnShape &w = WIDE ? a.wide : a.narrow;
+    const uint64_t cell = blockIdx.x;
+    const uint32_t slot = (uint32_t)(cell / a.heads), head = (uint32_t)(cell % a.heads);
+    // the row's tile, and how many parts its keys came in
+    AttnTile t;
+    uint32_t i;
+    if constexpr (WIDE) {
+        const int32_t r = find_request(a, slot, 1, 0);
+        if (r < 0 || !open_request(a, (uint32_t)r, t) || (uint32_t)t.n <= a.narrow_most) return;
+        i = slot - (uint32_t)t.first_row;
+    } else {
+        if (!open_request(a, slot / a.split_tokens, t) || (uint32_t)t.n > a.narrow_most || (uint32_t)t.n > a.split_tokens) return;
+        i = slot % a.split_tokens;
     }
-    const int32_t b0 = a.token_begin[lo], b1 = a.token_begin[lo + 1];
-    if (b1 < b0 || b1 <= (int32_t)row || (uint32_t)b1 > a.tokens || a.start[lo] < 0) return;
-    const uint32_t n = a.part_n[at];
-    if (n <= 1 || n > a.splits) return;
-    const uint64_t stride = (uint64_t)a.tokens * a.heads;
+    if (i >= (uint32_t)t.n) return;
+    open_tile(a, (int32_t)(i / w.tile_tokens * w.tile_tokens), w.tile_tokens, t);
+    const uint32_t n = parts_of(w, KeyTiles(t, WIDE ? (a.head_dim <= 128 ? 64 : 32) : kNarrowKeys).all);
+    if (n <= 1) return;
+    const uint64_t row = (uint64_t)t.first_row + i, stride = w.slots * a.heads;
+    const float *const lse = w.part_lse + cell, *const part = w.part_o + cell * a.head_dim;
     float M = -INFINITY;
-    for (uint32_t s = lane; s < n; s += 64) M = fmaxf(M, a.part_lse[s * stride + at]);
+    for (uint32_t s = tid; s < n; s += 256) M = fmaxf(M, lse[s * stride]);
 #pragma unroll
     for (int x = 1; x < 64; x *= 2) M = fmaxf(M, __shfl_xor(M, x));
+    if (lane == 0) s_top[tid >> 6] = M;
+    __syncthreads();
+    M = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
     const float base = M == -INFINITY ? 0.f : M;
-    float L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    for (uint32_t s = 0; s < n; ++s) {
-        const float w = __builtin_amdgcn_exp2f(a.part_lse[s * stride + at] - base);
-        L += w;
-        const float *p = a.part_o + (s * stride + at) * a.head_dim;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (lane + 64 * e < a.head_dim) o[e] += w * p[lane + 64 * e];
+    const uint32_t group = tid >> 5, piece = tid & 31;                             // head_dim / 4 pieces, two to a thread above 128
+    float L = 0.f;
+    f32x4 o[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll 4
+    for (uint32_t s = group; s < n; s += 8) {
+        const float share = __builtin_amdgcn_exp2f(lse[s * stride] - base);
+        L += share;
+        const float *p = part + s * stride * a.head_dim;
+        if (piece * 4 < a.head_dim) o[0] += share * *(const f32x4 *)(p + piece * 4);
+        if (piece * 4 + 128 < a.head_dim) o[1] += share * *(const f32x4 *)(p + piece * 4 + 128);
     }
-    const bool some = !(M == -INFINITY && L == 0.f);
-    const float inv = some ? 1.f / L : 0.f;
-    T *out = (T *)a.out + (int64_t)row * a.o_token + (int64_t)head * a.o_head;
+    s_o[group][piece] = o[0]; s_o[group][piece + 32] = o[1];
+    if (piece == 0) s_sum[group] = L;
+    __syncthreads();
+    L = 0.f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (lane + 64 * e < a.head_dim) out[lane + 64 * e] = (T)(some ? o[e] * inv : 0.f);
-    if (lane == 0 && a.lse) a.lse[at] = some ? (base + __builtin_amdgcn_logf(L)) * 0.69314718055994530942f : -INFINITY;
+    for (int k = 0; k < 8; ++k) L += s_sum[k];
+    const bool some = !(M == -INFINITY && L == 0.f);
+    if (tid < 64 && tid * 4 < a.head_dim) {
+        f32x4 x = s_o[0][tid];
+#pragma unroll
+        for (int k = 1; k < 8; ++k) x += s_o[k][tid];
+        const float inv = some ? 1.f / L : 0.f;
+        typedef typename AttnTypes<T>::x4 x4;
+        *(x4 *)((T *)a.out + (int64_t)row * a.o_token + (int64_t)head * a.o_head + tid * 4) =
+            x4{(T)(some ? x[0] * inv : 0.f), (T)(some ? x[1] * inv : 0.f), (T)(some ? x[2] * inv : 0.f), (T)(some ? x[3] * inv : 0.f)};
+    }
+    if (tid == 0 && a.lse) a.lse[row * a.heads + head] = some ? (base + __builtin_amdgcn_logf(L)) * 0.69314718055994530942f : -INFINITY;
 }
 
 }  // namespace srs

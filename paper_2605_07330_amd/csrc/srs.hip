@@ -670,43 +670,72 @@ int launch_rope(const RopeArgs &a, int dtype, uint32_t flags, hipStream_t st) {
 }  // namespace
 
 namespace {
+constexpr uint64_t kMaxKeys = 1ull << 30;              // of one request
+
 // How the attention of one call is laid out.
 struct AttnPlan {
-    uint32_t block, head_blocks, tile_tokens, tiles, splits, split_tiles;
+    AttnShape narrow, wide;
+    uint32_t narrow_most, split_tokens, wide_tiles;
     uint64_t workspace;
 };
 
-constexpr uint64_t kMaxKeys = 1ull << 30;              // of one request
+// Workgroups that a launch should have where rows are few: three of the narrow kernel's fit a CU, and four rounds even out requests of
+// unlike length; two of the wide one's.  And the fewest key tiles worth a workgroup.
+constexpr uint64_t kNarrowWorkgroups = 256 * 3 * 4, kWideWorkgroups = 256 * 2 * 2;
+constexpr uint64_t kLeastNarrowTiles = 2, kLeastWideTiles = 4;
 
-// Workgroups that a launch should have where rows are few: three of them fit a CU, and four rounds even out requests of unlike length.
-constexpr uint64_t kAttnWorkgroups = 256 * 3 * 4;
-constexpr uint32_t kLeastSplitTiles = 2;
+void attention_shape(AttnShape &w, uint32_t rows, uint32_t group, uint32_t key_step, uint64_t keys, uint32_t window, uint32_t sinks,
+                     uint64_t tiles, uint32_t kv_heads, uint64_t workgroups, uint64_t least) {
+    w.head_blocks = (group + rows - 1) / rows;
+    w.block = (group + w.head_blocks - 1) / w.head_blocks;
+    w.tile_tokens = rows / w.block;
+    uint64_t key_tiles = (keys + key_step - 1) / key_step;
+    if (window) {
+        const uint64_t seen = (sinks + key_step - 1) / key_step + ((uint64_t)window + w.tile_tokens + key_step - 1) / key_step + 1;
+        if (seen < key_tiles) key_tiles = seen;
+    }
+    const uint64_t units = tiles * kv_heads * w.head_blocks;
+    uint64_t each = (units * key_tiles + workgroups - 1) / workgroups;
+    each = each < least ? least : each;
+    const uint64_t splits = (key_tiles + each - 1) / each;
+    w.split_tiles = (uint32_t)each; w.splits = splits < 1 ? 1 : (uint32_t)splits;
+    w.part_o = w.part_lse = nullptr; w.slots = 0;
+}
 
 AttnPlan attention_plan(uint32_t nrequests, uint64_t tokens, uint32_t q_heads, uint32_t kv_heads, uint32_t head_dim, uint32_t table_width,
                         uint32_t page_tokens, uint32_t window, uint32_t sinks, uint64_t most_tokens, uint64_t most_keys) {
     AttnPlan p;
     const uint32_t group = q_heads / kv_heads;
-    p.head_blocks = (group + 15) / 16;
-    p.block = (group + p.head_blocks - 1) / p.head_blocks;
-    p.tile_tokens = 16 / p.block;
-    p.tiles = (uint32_t)(tokens / p.tile_tokens + nrequests);
     uint64_t keys = (uint64_t)table_width * page_tokens;
     if (most_keys && most_keys < keys) keys = most_keys;
-    uint64_t key_tiles = (keys + kNarrowKeys - 1) / kNarrowKeys;
-    if (window) {
-        const uint64_t seen = (sinks + kNarrowKeys - 1) / kNarrowKeys + ((uint64_t)window + p.tile_tokens + kNarrowKeys - 1) / kNarrowKeys + 1;
-        if (seen < key_tiles) key_tiles = seen;
-    }
-    const uint64_t busy = tokens < p.tiles ? tokens : p.tiles;             // tiles that hold something, at most
-    const uint64_t units = busy * kv_heads * p.head_blocks;
-    uint64_t each = (units * key_tiles + kAttnWorkgroups - 1) / kAttnWorkgroups;
-    each = each < kLeastSplitTiles ? kLeastSplitTiles : each;
-    uint64_t splits = (key_tiles + each - 1) / each;
-    if (splits < 1) splits = 1;
-    p.split_tiles = (uint32_t)each; p.splits = (uint32_t)splits;
-    p.workspace = splits > 1 ? tokens * q_heads * 4 * (splits * (head_dim + 1) + 1) : 0;
-    (void)most_tokens;
+    const uint64_t busy = tokens < nrequests ? tokens : nrequests;
+    attention_shape(p.narrow, 16, group, kNarrowKeys, keys, window, sinks, busy, kv_heads, kNarrowWorkgroups, kLeastNarrowTiles);
+    // A request whose new tokens fit one narrow tile is read once by it; the wide kernel takes the others, unless there are none.
+    const bool only_narrow = most_tokens && most_tokens <= p.narrow.tile_tokens;
+    p.narrow_most = only_narrow ? 0x7fffffffu : p.narrow.tile_tokens;
+    p.split_tokens = only_narrow ? (uint32_t)most_tokens : p.narrow.tile_tokens;
+    p.narrow.slots = (uint64_t)nrequests * p.split_tokens;
+    attention_shape(p.wide, 128, group, head_dim <= 128 ? 64 : 32, keys, window, sinks, 1, kv_heads, kWideWorkgroups, kLeastWideTiles);
+    const uint64_t wide_tiles = tokens / p.wide.tile_tokens + nrequests;
+    p.wide_tiles = only_narrow ? 0 : (uint32_t)wide_tiles;
+    // of the tiles, those that hold something: a request's last is the only one that may be less than full
+    const uint64_t full = tokens / p.wide.tile_tokens, chunks = tokens / (p.narrow.tile_tokens + 1);
+    const uint64_t wide_busy = full + (chunks < nrequests ? chunks : nrequests);
+    attention_shape(p.wide, 128, group, head_dim <= 128 ? 64 : 32, keys, window, sinks, wide_busy, kv_heads, kWideWorkgroups, kLeastWideTiles);
+    p.wide.slots = tokens;
+    if (only_narrow) p.wide.splits = 1;
+    p.workspace = 0;
+    if (p.narrow.splits > 1) p.workspace += p.narrow.splits * p.narrow.slots * q_heads * 4 * (head_dim + 4);
+    if (p.wide.splits > 1) p.workspace += p.wide.splits * p.wide.slots * q_heads * 4 * (head_dim + 4);
     return p;
+}
+
+// Where the parts lie in the workspace: results, then their lse (four words' room for each, which keeps what follows aligned).
+void attention_parts(AttnShape &w, uint32_t q_heads, uint32_t head_dim, float *&at) {
+    if (w.splits <= 1) return;
+    const uint64_t cells = w.splits * w.slots * q_heads;
+    w.part_o = at; w.part_lse = at + cells * head_dim;
+    at += cells * (head_dim + 4);
 }
 
 // Pages that hold whole blocks of 16 keys, whose rows a 32-bit offset spans: addresses are then scalar but for that offset.
@@ -716,23 +745,37 @@ bool in_blocks(const srs_cache *c) {
 }
 
 template <class T, int DP>
-int launch_attention(const AttnArgs &a, bool blocks, uint32_t grid, hipStream_t st) {
-    if (blocks && a.head_dim == DP) hipLaunchKernelGGL((attention_narrow_kernel<T, DP, true, true>), dim3(grid), dim3(256), 0, st, a);
-    else if (blocks) hipLaunchKernelGGL((attention_narrow_kernel<T, DP, true, false>), dim3(grid), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((attention_narrow_kernel<T, DP, false, false>), dim3(grid), dim3(256), 0, st, a);
-    SRS_HIP(hipGetLastError());
-    if (a.splits > 1) {
-        hipLaunchKernelGGL((attention_join_kernel<T>), dim3((uint32_t)(((uint64_t)a.tokens * a.heads + 3) / 4)), dim3(256), 0, st, a);
+int launch_attention(const AttnArgs &a, bool blocks, hipStream_t st) {
+    const dim3 narrow(a.nrequests * a.narrow.splits * a.kv_heads * a.narrow.head_blocks), wide(a.wide_tiles * a.wide.splits * a.kv_heads * a.wide.head_blocks);
+#define SRS_ATTENTION(BLOCKS, EXACT)                                                                                    \
+    do {                                                                                                                \
+        if (a.wide_tiles) {                                                                                             \
+            hipLaunchKernelGGL((attention_wide_kernel<T, DP, BLOCKS, EXACT>), wide, dim3(256), 0, st, a);               \
+            SRS_HIP(hipGetLastError());                                                                                 \
+        }                                                                                                               \
+        hipLaunchKernelGGL((attention_narrow_kernel<T, DP, BLOCKS, EXACT>), narrow, dim3(256), 0, st, a);               \
+        SRS_HIP(hipGetLastError());                                                                                     \
+    } while (0)
+    if (blocks && a.head_dim == DP) SRS_ATTENTION(true, true);
+    else if (blocks) SRS_ATTENTION(true, false);
+    else SRS_ATTENTION(false, false);
+#undef SRS_ATTENTION
+    if (a.narrow.splits > 1) {
+        hipLaunchKernelGGL((attention_join_kernel<T, false>), dim3((uint32_t)(a.narrow.slots * a.heads)), dim3(256), 0, st, a);
+        SRS_HIP(hipGetLastError());
+    }
+    if (a.wide.splits > 1) {
+        hipLaunchKernelGGL((attention_join_kernel<T, true>), dim3((uint32_t)(a.wide.slots * a.heads)), dim3(256), 0, st, a);
         SRS_HIP(hipGetLastError());
     }
     return SRS_OK;
 }
 
 template <class T>
-int launch_attention(const AttnArgs &a, bool blocks, uint32_t grid, hipStream_t st) {
-    if (a.head_dim <= 64) return launch_attention<T, 64>(a, blocks, grid, st);
-    if (a.head_dim <= 128) return launch_attention<T, 128>(a, blocks, grid, st);
-    return launch_attention<T, 256>(a, blocks, grid, st);
+int launch_attention(const AttnArgs &a, bool blocks, hipStream_t st) {
+    if (a.head_dim <= 64) return launch_attention<T, 64>(a, blocks, st);
+    if (a.head_dim <= 128) return launch_attention<T, 128>(a, blocks, st);
+    return launch_attention<T, 256>(a, blocks, st);
 }
 }  // namespace
 
@@ -1461,8 +1504,9 @@ int srs_cache_attention(srs_ctx *ctx, const srs_cache *cache, const srs_rows *q,
     const AttnPlan p = attention_plan(nrequests, tokens, q->heads, cache->heads, cache->head_dim, table_width, cache->page_tokens, window, sinks,
                                       most_tokens, most_keys);
     if (p.workspace && (!workspace || ((uintptr_t)workspace & 15u) || workspace_bytes < p.workspace)) return SRS_ERR_INVALID;
-    const uint64_t grid = (uint64_t)p.tiles * p.splits * cache->heads * p.head_blocks;
-    if (grid > 0x7fffffffull || tokens * q->heads > 0x7fffffffull) return SRS_ERR_INVALID;
+    if ((uint64_t)nrequests * p.narrow.splits * cache->heads * p.narrow.head_blocks > 0x7fffffffull || p.narrow.slots * q->heads > 0x7fffffffull ||
+        (uint64_t)p.wide_tiles * p.wide.splits * cache->heads * p.wide.head_blocks > 0x7fffffffull || tokens * q->heads > 0x7fffffffull)
+        return SRS_ERR_INVALID;
     hipStream_t st = (hipStream_t)stream;
     SRS_ON_DEVICE(ctx->device);
     AttnArgs a;
@@ -1474,18 +1518,20 @@ int srs_cache_attention(srs_ctx *ctx, const srs_cache *cache, const srs_rows *q,
     a.v_page = cache->v_page; a.v_token = cache->v_token; a.v_head = cache->v_head;
     a.token_begin = token_begin; a.start = start; a.table = table;
     a.tokens = (uint32_t)tokens; a.nrequests = nrequests; a.width = table_width; a.page = cache->page_tokens; a.pages = cache->pages;
-    a.page_shift = 32;
-    for (uint32_t k = 0; k < 31; ++k)
-        if (cache->page_tokens == 1u << k) a.page_shift = k;
+    uint32_t log = 0;                                   // ceil(log2(page)): the quotient is exact for numerators below 2^31
+    while ((1ull << log) < cache->page_tokens) ++log;
+    a.page_magic = (uint32_t)(((1ull << (31 + log)) + cache->page_tokens - 1) / cache->page_tokens); a.page_shift = 31 + log;
     a.heads = q->heads; a.kv_heads = cache->heads; a.head_dim = cache->head_dim; a.group = q->heads / cache->heads;
-    a.window = window; a.sinks = sinks; a.scale = scale * 1.44269504088896340736f; a.full = (flags & SRS_ATTN_FULL) != 0; a.flags = ctx->flags;
-    a.block = p.block; a.head_blocks = p.head_blocks; a.tile_tokens = p.tile_tokens; a.tiles = p.tiles;
-    a.splits = p.splits; a.split_tiles = p.split_tiles;
-    const uint64_t cells = tokens * q->heads;
-    a.part_o = (float *)workspace; a.part_lse = a.part_o + p.splits * cells * cache->head_dim; a.part_n = (uint32_t *)(a.part_lse + p.splits * cells);
+    a.window = window; a.sinks = sinks; a.full = (flags & SRS_ATTN_FULL) != 0; a.flags = ctx->flags;
+    a.scale = scale == 0.f ? 1.f : std::fabs(scale) * 1.44269504088896340736f;
+    a.sign = scale > 0.f ? 1.f : scale < 0.f ? -1.f : 0.f;
+    a.narrow = p.narrow; a.wide = p.wide; a.narrow_most = p.narrow_most; a.split_tokens = p.split_tokens; a.wide_tiles = p.wide_tiles;
+    float *at = (float *)workspace;
+    attention_parts(a.narrow, q->heads, cache->head_dim, at);
+    attention_parts(a.wide, q->heads, cache->head_dim, at);
     const bool blocks = in_blocks(cache);
-    if (cache->dtype == SRS_BF16) return launch_attention<__bf16>(a, blocks, (uint32_t)grid, st);
-    return launch_attention<_Float16>(a, blocks, (uint32_t)grid, st);
+    if (cache->dtype == SRS_BF16) return launch_attention<__bf16>(a, blocks, st);
+    return launch_attention<_Float16>(a, blocks, st);
 }
 
 // ---------------------------------------------------------------------------------------------
