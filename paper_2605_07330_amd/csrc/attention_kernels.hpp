@@ -208,10 +208,11 @@ __device__ __forceinline__ uint32_t parts_of(const AttnShape &w, int32_t all) {
 
 // ---- few rows: decoding ------------------------------------------------------------------------------------------------------
 // 16 rows to a workgroup, 32 keys of a tile of 128 to each of its four waves, which join their results at the end.  Scores come as
-// K Q^T (keys down, rows across: v_mfma 16x16x32, keys straight from memory in the operand's own layout), so that a lane holds
-// the weights of one row for eight keys, which is how the second product V^T P^T takes them if its keys are counted in the
-// same order.  V passes through LDS, wave by wave, for its transposed read; its 16-byte pieces are rearranged in each row so that eight
-// rows' reads fall on all banks.  The next tile's rows are in flight meanwhile.
+// K Q^T (keys down, rows across: v_mfma 16x16x32), so that a lane holds the weights of one row for eight keys, which is how the second
+// product V^T P^T takes them if its keys are counted in the same order.  K and V pass through LDS, wave by wave: V for its transposed
+// read, K so that memory is read by whole rows, past the caches (128 requests of up to 8192 keys: 464 us with K straight from
+// memory in the operand's layout, half a line to an instruction, where the hint did nothing; 417 this way).  Pieces of 16 bytes are rearranged
+// in each row so that neither read meets itself on a bank.  The next tile's rows are in flight meanwhile.
 // Bound: the cache's bytes.  Weights meet the values in two parts (value and remainder of its rounding): the second product costs
 // nothing here.
 constexpr int kNarrowKeys = 128;
@@ -220,8 +221,9 @@ template <class T, int DP, bool BLOCKS, bool EXACT>
 __global__ __launch_bounds__(256, DP == 64 ? 3 : DP == 128 ? 2 : 1) void attention_narrow_kernel(const AttnArgs a) {
     typedef typename AttnTypes<T>::x8 x8;
     typedef typename AttnTypes<T>::x4 x4;
-    constexpr int kQC = DP / 32, kVC = DP / 16, kRegion = 64 * DP + 256, kRowPieces = DP / 8;      // pieces of 16 bytes
+    constexpr int kQC = DP / 32, kVC = DP / 16, kRegion = 64 * DP + 256, kRowPieces = DP / 8;      // 32 rows of V, or 16 of float results; pieces of 16 bytes
     __shared__ __attribute__((aligned(16))) unsigned char s_mem[4 * kRegion];
+    __shared__ __attribute__((aligned(16))) unsigned char s_keys[4][64 * DP];
     __shared__ float s_m[4][16], s_l[4][16];
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform_value(tid >> 6), g = lane >> 4, n = lane & 15;
     const AttnShape &w = a.narrow;
@@ -266,11 +268,13 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : DP == 128 ? 2 : 1) void attenti
         }
     }
 
-    // Where this lane's pieces lie behind the base of a block of 16 keys: of K the row of key n, piece g of every 32 elements; of V
-    // piece vpiece of row vrow of every kRowsPerLoad.  Pieces behind the head's end are read from its beginning and dropped.
+    // This lane carries piece `piece` of row my_row of every kRowsPerLoad of K and of V: whole rows go out in one load instruction.  Pieces
+    // behind the head's end are read from its beginning and dropped.
     constexpr int kRowsPerLoad = 64 / kRowPieces;
-    const uint32_t vpiece = lane % kRowPieces, vrow = lane / kRowPieces;
-    const uint32_t k_lane = n * (uint32_t)a.k_token * 2 + g * 16, v_lane = vrow * (uint32_t)a.v_token * 2 + (EXACT || vpiece * 8 < a.head_dim ? vpiece * 16 : 0);
+    const uint32_t piece = lane % kRowPieces, my_row = lane / kRowPieces;
+    const bool inside = EXACT || piece * 8 < a.head_dim;
+    const uint32_t piece_off = inside ? piece * 16 : 0;
+    const uint32_t k_lane = my_row * (uint32_t)a.k_token * 2 + piece_off, v_lane = my_row * (uint32_t)a.v_token * 2 + piece_off;
     const unsigned char *const k_base = a.k + (int64_t)kh * a.k_head * 2, *const v_base = a.v + (int64_t)kh * a.v_head * 2;
     const const_i32 *const table = (const const_i32 *)(a.table + (int64_t)t.r * a.width);
 
@@ -304,49 +308,29 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : DP == 128 ? 2 : 1) void attenti
         p.ok = ok;
         return p;
     };
-    x8 kreg[2][kQC];
-    u32x4 vreg[kVC];
-    auto load_k = [&](const Pages &pg) {
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            gptr<const unsigned char> p;
-            uint32_t off = k_lane;
-            if constexpr (BLOCKS) {
-                p = scalar_base(as_global(k_base + ((int64_t)pg.page[b] * a.k_page + (int64_t)pg.place[b] * a.k_token) * 2));
-            } else {
-                p = as_global(k_base + ((int64_t)__shfl(pg.page[0], 16 * b + n) * a.k_page + (int64_t)__shfl(pg.place[0], 16 * b + n) * a.k_token) * 2);
-                off = g * 16;
-            }
-#pragma unroll
-            for (int c = 0; c < kQC; ++c) {
-                if constexpr (EXACT) {
-                    kreg[b][c] = *(gptr<const x8>)(p + off + c * 64);
-                } else {
-                    const bool inside = c * 32 + g * 8 < a.head_dim;
-                    const u32x4 x = *(gptr<const u32x4>)(p + (inside ? off + c * 64 : off - g * 16));
-                    const u32x4 y = {inside ? x[0] : 0u, inside ? x[1] : 0u, inside ? x[2] : 0u, inside ? x[3] : 0u};
-                    kreg[b][c] = __builtin_bit_cast(x8, y);
-                }
-            }
-        }
-    };
-    auto load_v = [&](const Pages &pg) {
+    u32x4 kreg[kVC], vreg[kVC];
+    auto load_rows = [&](const Pages &pg, const unsigned char *base, int64_t page_stride, int64_t token_stride, uint32_t lane_off, u32x4 (&to)[kVC]) {
 #pragma unroll
         for (int c = 0; c < kVC; ++c) {
             constexpr int kLoads = 16 / kRowsPerLoad;                               // of a block
             if constexpr (BLOCKS) {
                 const int b = c / kLoads;
-                const auto p = scalar_base(as_global(v_base + ((int64_t)pg.page[b] * a.v_page + ((int64_t)pg.place[b] + (c % kLoads) * kRowsPerLoad) * a.v_token) * 2));
-                vreg[c] = *(gptr<const u32x4>)(p + v_lane);
+                const auto p = scalar_base(as_global(base + ((int64_t)pg.page[b] * page_stride + ((int64_t)pg.place[b] + (c % kLoads) * kRowsPerLoad) * token_stride) * 2));
+                to[c] = __builtin_nontemporal_load((gptr<const u32x4>)(p + lane_off));
             } else {
-                const uint32_t k = c * kRowsPerLoad + vrow;
-                const auto p = as_global(v_base + ((int64_t)__shfl(pg.page[0], k) * a.v_page + (int64_t)__shfl(pg.place[0], k) * a.v_token) * 2);
-                vreg[c] = *(gptr<const u32x4>)(p + (v_lane - vrow * (uint32_t)a.v_token * 2));
+                const uint32_t k = c * kRowsPerLoad + my_row;
+                const auto p = as_global(base + ((int64_t)__shfl(pg.page[0], k) * page_stride + (int64_t)__shfl(pg.place[0], k) * token_stride) * 2);
+                to[c] = __builtin_nontemporal_load((gptr<const u32x4>)(p + piece_off));
             }
         }
     };
-    unsigned char *const mine = s_mem + wave * kRegion;
-    auto place_of = [&](uint32_t key, uint32_t piece) { return key * (DP * 2) + ((piece ^ ((key & 7) << 1)) & (kRowPieces - 1)) * 16; };
+    auto load = [&](const Pages &pg) {
+        load_rows(pg, v_base, a.v_page, a.v_token, v_lane, vreg);
+        load_rows(pg, k_base, a.k_page, a.k_token, k_lane, kreg);
+    };
+    unsigned char *const mine = s_mem + wave * kRegion, *const keys = s_keys[wave];
+    auto place_of = [&](uint32_t key, uint32_t p) { return key * (DP * 2) + ((p ^ ((key & 7) << 1)) & (kRowPieces - 1)) * 16; };
+    auto k_place = [&](uint32_t key, uint32_t p) { return key * (DP * 2) + (p ^ (DP == 64 ? (key >> 1) & 7 : key & 15)) * 16; };
     f32x4 o[kVC];
 #pragma unroll
     for (int c = 0; c < kVC; ++c) o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -356,7 +340,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : DP == 128 ? 2 : 1) void attenti
     if (from < to) {
     Pages now = take(ask(tiles.key(from, kNarrowKeys) + shift, from < to));
     Questions next = ask(tiles.key(from + 1, kNarrowKeys) + shift, from + 1 < to);
-    load_v(now); load_k(now);
+    load(now);
 #pragma unroll 1
     for (int32_t i = from; i < to; ++i) {
         const int32_t key = tiles.key(i, kNarrowKeys) + shift;
@@ -368,7 +352,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : DP == 128 ? 2 : 1) void attenti
             const uint32_t any = (uint32_t)seen_bits(key, t.low, t.end, t.sinks) & now.ok;
 #pragma unroll
             for (int c = 0; c < kVC; ++c) {
-                const bool here = any >> (c * kRowsPerLoad + vrow) & 1u;
+                const bool here = any >> (c * kRowsPerLoad + my_row) & 1u;
                 vreg[c] = u32x4{here ? vreg[c][0] : 0u, here ? vreg[c][1] : 0u, here ? vreg[c][2] : 0u, here ? vreg[c][3] : 0u};
             }
         }
@@ -383,21 +367,24 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : DP == 128 ? 2 : 1) void attenti
             for (int c = 0; c < kVC; ++c) vreg[c] = finite_values<T>(vreg[c]);
         }
 #pragma unroll
-        for (int c = 0; c < kVC; ++c) *(u32x4 *)(mine + place_of(c * kRowsPerLoad + vrow, vpiece)) = vreg[c];
+        for (int c = 0; c < kVC; ++c) {
+            *(u32x4 *)(mine + place_of(c * kRowsPerLoad + my_row, piece)) = vreg[c];
+            if constexpr (EXACT) *(u32x4 *)(keys + k_place(c * kRowsPerLoad + my_row, piece)) = kreg[c];
+            else *(u32x4 *)(keys + k_place(c * kRowsPerLoad + my_row, piece)) = u32x4{inside ? kreg[c][0] : 0u, inside ? kreg[c][1] : 0u, inside ? kreg[c][2] : 0u, inside ? kreg[c][3] : 0u};
+        }
         const uint32_t ok = now.ok;
         now = take(next);
         next = ask(tiles.key(i + 2, kNarrowKeys) + shift, i + 2 < to);
-        if (more) load_v(now);
+        if (more) load(now);
         float x[8], top = -INFINITY;
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int c = 0; c < kQC; ++c) s = mfma_16x16x32(kreg[b][c], q[c], s);
+            for (int c = 0; c < kQC; ++c) s = mfma_16x16x32(*(const x8 *)(keys + k_place(16 * b + n, 4 * c + g)), q[c], s);
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[4 * b + e] = s[e] * a.scale;
         }
-        if (more) load_k(now);
         if (!whole) {
             const uint32_t sees = ((uint32_t)seen_bits(key, row_low, row_end, t.sinks) & ok) >> (4 * g);
 #pragma unroll

@@ -679,9 +679,11 @@ struct AttnPlan {
     uint64_t workspace;
 };
 
-// Workgroups that a launch should have where rows are few: three of the narrow kernel's fit a CU, and four rounds even out requests of
-// unlike length; two of the wide one's.  And the fewest key tiles worth a workgroup.
-constexpr uint64_t kNarrowWorkgroups = 256 * 3 * 4, kWideWorkgroups = 256 * 2 * 2;
+// Workgroups that a launch should have where rows are few (two of either kernel fit a CU).  The narrow kernel's are short and even
+// out requests of unlike length; more are not worth their beginning and end (1536 / 3072 / 6144, us: 128 requests of up to 8192 keys 580 /
+// 464 / 472, two of up to 131072 136 / 138 / 164).  The wide kernel's parts cost a pass over all results: none where the card is nearly
+// full without (528 workgroups of 35 key tiles in two parts 166 us and 109 to join).  And the fewest key tiles worth a workgroup.
+constexpr uint64_t kNarrowWorkgroups = 3072, kWideWorkgroups = 512;
 constexpr uint64_t kLeastNarrowTiles = 2, kLeastWideTiles = 4;
 
 void attention_shape(AttnShape &w, uint32_t rows, uint32_t group, uint32_t key_step, uint64_t keys, uint32_t window, uint32_t sinks,
@@ -695,7 +697,7 @@ void attention_shape(AttnShape &w, uint32_t rows, uint32_t group, uint32_t key_s
         if (seen < key_tiles) key_tiles = seen;
     }
     const uint64_t units = tiles * kv_heads * w.head_blocks;
-    uint64_t each = (units * key_tiles + workgroups - 1) / workgroups;
+    uint64_t each = units * 4 >= workgroups * 3 && rows > 16 ? key_tiles : (units * key_tiles + workgroups - 1) / workgroups;
     each = each < least ? least : each;
     const uint64_t splits = (key_tiles + each - 1) / each;
     w.split_tiles = (uint32_t)each; w.splits = splits < 1 ? 1 : (uint32_t)splits;
