@@ -194,6 +194,7 @@ struct RopeArgs {
     uint64_t places;                // pages * page
     uint32_t page;
     uint32_t tokens, head_dim, rot;
+    uint32_t shares;                // workgroups to a token
     const int32_t *positions;
     const double *inv_freq;
     float magnitude;
@@ -208,55 +209,141 @@ __device__ __forceinline__ void turn_of(int32_t position, double inv_freq, float
     sincospif(half_turns, &s, &c);
 }
 
-// One thread per pair, or per element that is copied.
-template <class T, bool INTERLEAVED>
-__global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a, bool transpose) {
-    const uint32_t units = a.rot / 2 + (a.head_dim - a.rot);
-    const uint32_t heads = a.x.heads + a.k.heads + a.v.heads;
-    const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= (uint64_t)a.tokens * heads * units) return;
-    const uint32_t u = (uint32_t)(i % units), head = (uint32_t)(i / units % heads), t = (uint32_t)(i / units / heads);
-    const T *from;
-    T *to;
-    bool turned = true;
+// Where row t's head `head` (queries, then keys, then values) comes from and goes to; whether it is turned.  Nothing where its slot is none.
+template <class T>
+__device__ __forceinline__ bool rope_row(const RopeArgs &a, uint32_t t, uint32_t head, int64_t page, int64_t place, bool slot_ok, const T *&from, T *&to, bool &turned) {
+    turned = true;
     if (head < a.x.heads) {
         from = (const T *)a.x.p + (int64_t)t * a.x.token_stride + (int64_t)head * a.x.head_stride;
         to = (T *)a.out.p + (int64_t)t * a.out.token_stride + (int64_t)head * a.out.head_stride;
+        return true;
+    }
+    if (!slot_ok) return false;
+    uint32_t h = head - a.x.heads;
+    if (h < a.k.heads) {
+        from = (const T *)a.k.p + (int64_t)t * a.k.token_stride + (int64_t)h * a.k.head_stride;
+        to = (T *)a.k_cache + page * a.k_page + place * a.k_token + (int64_t)h * a.k_head;
     } else {
-        const int64_t slot = a.slots[t];
-        if (slot < 0 || (uint64_t)slot >= a.places) {
-            if (slot != -1) atomicOr(a.flags, kFlagBadIndex);
-            return;
-        }
-        const int64_t page = slot / a.page, place = slot % a.page;
-        if (head < a.x.heads + a.k.heads) {
-            const uint32_t h = head - a.x.heads;
-            from = (const T *)a.k.p + (int64_t)t * a.k.token_stride + (int64_t)h * a.k.head_stride;
-            to = (T *)a.k_cache + page * a.k_page + place * a.k_token + (int64_t)h * a.k_head;
-        } else {
-            const uint32_t h = head - a.x.heads - a.k.heads;
-            from = (const T *)a.v.p + (int64_t)t * a.v.token_stride + (int64_t)h * a.v.head_stride;
-            to = (T *)a.v_cache + page * a.v_page + place * a.v_token + (int64_t)h * a.v_head;
-            turned = false;
-        }
+        h -= a.k.heads;
+        from = (const T *)a.v.p + (int64_t)t * a.v.token_stride + (int64_t)h * a.v.head_stride;
+        to = (T *)a.v_cache + page * a.v_page + place * a.v_token + (int64_t)h * a.v_head;
+        turned = false;
     }
-    if (u >= a.rot / 2) {
-        const uint32_t d = a.rot + (u - a.rot / 2);
-        to[d] = from[d];
-        return;
+    return true;
+}
+
+__device__ __forceinline__ bool rope_slot(const RopeArgs &a, uint32_t t, int64_t &page, int64_t &place) {
+    page = place = 0;
+    if (!a.slots) return false;
+    const int64_t slot = a.slots[t];
+    if (slot < 0 || (uint64_t)slot >= a.places) {
+        if (slot != -1 && threadIdx.x == 0) atomicOr(a.flags, kFlagBadIndex);
+        return false;
     }
-    const uint32_t d1 = INTERLEAVED ? 2 * u : u, d2 = INTERLEAVED ? 2 * u + 1 : u + a.rot / 2;
-    if (!turned) {
+    page = slot / a.page; place = slot - page * a.page;
+    return true;
+}
+
+// Any strides, alignment and sizes: one thread per pair, or per element that is copied.
+template <class T, bool INTERLEAVED>
+__global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a, bool transpose) {
+    const uint32_t units = a.rot / 2 + (a.head_dim - a.rot), heads = a.x.heads + a.k.heads + a.v.heads;
+    const uint32_t t = blockIdx.x / a.shares;
+    int64_t page, place;
+    const bool slot_ok = rope_slot(a, t, page, place);
+    for (uint32_t i = (blockIdx.x % a.shares) * 256 + threadIdx.x; i < heads * units; i += a.shares * 256) {
+        const uint32_t head = i / units, u = i % units;
+        const T *from;
+        T *to;
+        bool turned;
+        if (!rope_row(a, t, head, page, place, slot_ok, from, to, turned)) continue;
+        if (u >= a.rot / 2) {
+            const uint32_t d = a.rot + (u - a.rot / 2);
+            to[d] = from[d];
+            continue;
+        }
+        const uint32_t d1 = INTERLEAVED ? 2 * u : u, d2 = INTERLEAVED ? 2 * u + 1 : u + a.rot / 2;
         const T x1 = from[d1], x2 = from[d2];
-        to[d1] = x1; to[d2] = x2;
-        return;
+        float c = 1.f, s = 0.f;
+        if (turned) {
+            turn_of(a.positions[t], a.inv_freq[u], c, s);
+            c *= a.magnitude; s *= transpose ? -a.magnitude : a.magnitude;
+        }
+        to[d1] = turned ? (T)((float)x1 * c - (float)x2 * s) : x1;
+        to[d2] = turned ? (T)((float)x2 * c + (float)x1 * s) : x2;
     }
-    float c, s;
-    turn_of(a.positions[t], a.inv_freq[u], c, s);
-    c *= a.magnitude; s *= transpose ? -a.magnitude : a.magnitude;
-    const float x1 = (float)from[d1], x2 = (float)from[d2];
-    to[d1] = (T)(x1 * c - x2 * s);
-    to[d2] = (T)(x2 * c + x1 * s);
+}
+
+// Rows in 16-byte pieces: a workgroup takes a token, or a share of its heads where there are few tokens.  Its sines and cosines are
+// worked out once, a thread each, while the first pieces are on their way, and serve all heads from LDS; a thread then turns
+// the two pieces that hold a run of pairs (or the one, interleaved).  Bound: memory.  One thread per pair and head, each with
+// its own sine, took twice as long: 8192 tokens of 40 heads of 128 80 us (4.2 and 2.1 TB/s, read and written).
+constexpr uint32_t kTurns = 512;                            // pairs that the table holds
+
+template <class T, bool INTERLEAVED>
+__global__ __launch_bounds__(256) void rope_pieces_kernel(const RopeArgs a, bool transpose) {
+    constexpr int N = 16 / sizeof(T), kAhead = 2;           // elements of a piece; units of a thread in flight
+    typedef T piece __attribute__((ext_vector_type(N)));
+    __shared__ __attribute__((aligned(16))) float s_cos[kTurns], s_sin[kTurns];
+    const uint32_t turning = INTERLEAVED ? a.rot / N : a.rot / 2 / N, units = turning + (a.head_dim - a.rot) / N, heads = a.x.heads + a.k.heads + a.v.heads;
+    const uint32_t t = blockIdx.x / a.shares, step = a.shares * 256;
+    int64_t page, place;
+    const bool slot_ok = rope_slot(a, t, page, place);
+    struct Unit { T *to; piece x, y; uint32_t d; bool there, turns, turned; };
+    auto open = [&](uint32_t i) {
+        Unit z;
+        const uint32_t head = i / units, u = i - head * units;
+        const T *from = nullptr;
+        z.there = i < heads * units && rope_row(a, t, head, page, place, slot_ok, from, z.to, z.turned);
+        z.turns = u < turning;
+        z.d = z.turns ? u * N : a.rot + (u - turning) * N;
+        if (z.there) {
+            z.x = *(const piece *)(from + z.d);
+            if (!INTERLEAVED && z.turns) z.y = *(const piece *)(from + z.d + a.rot / 2);
+        }
+        return z;
+    };
+    auto close = [&](const Unit &z) {
+        if (!z.there) return;
+        piece x = z.x, y = z.y;
+        if (z.turns && z.turned) {
+            if constexpr (INTERLEAVED) {
+#pragma unroll
+                for (int e = 0; e < N; e += 2) {
+                    const float c = s_cos[z.d / 2 + e / 2], s = s_sin[z.d / 2 + e / 2], x1 = (float)z.x[e], x2 = (float)z.x[e + 1];
+                    x[e] = (T)(x1 * c - x2 * s);
+                    x[e + 1] = (T)(x2 * c + x1 * s);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const float c = s_cos[z.d + e], s = s_sin[z.d + e], x1 = (float)z.x[e], x2 = (float)z.y[e];
+                    x[e] = (T)(x1 * c - x2 * s);
+                    y[e] = (T)(x2 * c + x1 * s);
+                }
+            }
+        }
+        *(piece *)(z.to + z.d) = x;
+        if (!INTERLEAVED && z.turns) *(piece *)(z.to + z.d + a.rot / 2) = y;
+    };
+    uint32_t i = (blockIdx.x % a.shares) * 256 + threadIdx.x;
+    Unit z[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) z[k] = open(i + k * step);
+    for (uint32_t u = threadIdx.x; u < a.rot / 2; u += 256) {
+        float c, s;
+        turn_of(a.positions[t], a.inv_freq[u], c, s);
+        s_cos[u] = c * a.magnitude; s_sin[u] = s * (transpose ? -a.magnitude : a.magnitude);
+    }
+    __syncthreads();
+    while (true) {
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) close(z[k]);
+        i += kAhead * step;
+        if (i >= heads * units) break;
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) z[k] = open(i + k * step);
+    }
 }
 
 }  // namespace srs

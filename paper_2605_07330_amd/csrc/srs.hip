@@ -649,16 +649,36 @@ bool rotation_ok(uint32_t rot_dim, uint32_t head_dim, uint32_t flags, const int3
     return positions && inv_freq && !((uintptr_t)positions & 3u) && !((uintptr_t)inv_freq & 7u) && std::isfinite(magnitude);
 }
 
-int launch_rope(const RopeArgs &a, int dtype, uint32_t flags, hipStream_t st) {
-    const uint64_t n = (uint64_t)a.tokens * (a.x.heads + a.k.heads + a.v.heads) * (a.rot / 2 + (a.head_dim - a.rot));
-    if (n == 0) return SRS_OK;
-    const uint64_t blocks = (n + 255) / 256;
+// Do all rows and strides let 16-byte pieces be read and written, and whole pieces be turned?
+bool rope_in_pieces(const RopeArgs &a, uint32_t size, bool interleaved) {
+    const uint32_t n = 16 / size;
+    if (a.head_dim % n || a.rot % (interleaved ? n : 2 * n) || a.rot / 2 > kTurns) return false;
+    auto rows = [n](const RowsArg &r) { return r.heads == 0 || (((uintptr_t)r.p & 15u) == 0 && r.token_stride % n == 0 && r.head_stride % n == 0); };
+    if (!rows(a.x) || !rows(a.out) || !rows(a.k) || !rows(a.v)) return false;
+    if (!a.slots) return true;
+    return (((uintptr_t)a.k_cache | (uintptr_t)a.v_cache) & 15u) == 0 &&
+           ((a.k_page | a.k_token | a.k_head | a.v_page | a.v_token | a.v_head) & (int64_t)(n - 1)) == 0;
+}
+
+int launch_rope(RopeArgs &a, int dtype, uint32_t flags, hipStream_t st) {
+    const uint32_t size = elem_bytes(dtype);
+    const bool transpose = (flags & SRS_ROPE_TRANSPOSE) != 0, interleaved = (flags & SRS_ROPE_INTERLEAVED) != 0;
+    const bool pieces = rope_in_pieces(a, size, interleaved);
+    const uint64_t heads = (uint64_t)a.x.heads + a.k.heads + a.v.heads;
+    const uint64_t each = !pieces ? a.rot / 2 + (a.head_dim - a.rot) : (interleaved ? a.rot : a.rot / 2) / (16 / size) + (a.head_dim - a.rot) / (16 / size);
+    if (heads * each > 0x7fffffffull - 65536) return SRS_ERR_INVALID;
+    // a workgroup for a token; where that leaves CUs idle, for as much of one as its threads take at once
+    const uint64_t most = (heads * each + 255) / 256, wanted = (1024 + a.tokens - 1) / a.tokens;
+    a.shares = (uint32_t)(most < wanted ? most : wanted);
+    const uint64_t blocks = (uint64_t)a.tokens * a.shares;
     if (blocks > 0x7fffffffull) return SRS_ERR_INVALID;
-    const bool transpose = (flags & SRS_ROPE_TRANSPOSE) != 0;
-#define SRS_ROPE_LAUNCH(T)                                                                                                       \
-    do {                                                                                                                         \
-        if (flags & SRS_ROPE_INTERLEAVED) hipLaunchKernelGGL((rope_kernel<T, true>), dim3((uint32_t)blocks), dim3(256), 0, st, a, transpose); \
-        else hipLaunchKernelGGL((rope_kernel<T, false>), dim3((uint32_t)blocks), dim3(256), 0, st, a, transpose);                 \
+#define SRS_ROPE_LAUNCH(T)                                                                                                      \
+    do {                                                                                                                        \
+        const dim3 grid((uint32_t)blocks);                                                                                      \
+        if (pieces && interleaved) hipLaunchKernelGGL((rope_pieces_kernel<T, true>), grid, dim3(256), 0, st, a, transpose);     \
+        else if (pieces) hipLaunchKernelGGL((rope_pieces_kernel<T, false>), grid, dim3(256), 0, st, a, transpose);              \
+        else if (interleaved) hipLaunchKernelGGL((rope_kernel<T, true>), grid, dim3(256), 0, st, a, transpose);                 \
+        else hipLaunchKernelGGL((rope_kernel<T, false>), grid, dim3(256), 0, st, a, transpose);                                 \
     } while (0)
     if (dtype == SRS_BF16) SRS_ROPE_LAUNCH(__bf16);
     else if (dtype == SRS_FP16) SRS_ROPE_LAUNCH(_Float16);
