@@ -20,8 +20,19 @@ struct TablesArgs {
     int64_t *slots;
     int32_t *positions;
     uint32_t max_tokens;
-    uint32_t *flags;
+    uint32_t *flags, *ticket;
 };
+
+// Whether this workgroup is the last of the launch to come here; the counter is 0 again afterwards.  What the others have read before
+// is then theirs to overwrite.
+__device__ __forceinline__ bool last_workgroup(uint32_t *ticket) {
+    __shared__ uint32_t s_last;
+    if (gridDim.x == 1) return true;
+    __syncthreads();
+    if (threadIdx.x == 0) s_last = atomicInc(ticket, gridDim.x - 1) == gridDim.x - 1;
+    __syncthreads();
+    return s_last != 0;
+}
 
 // Exclusive sums of two numbers per thread over the workgroup; totals in the last two.
 __device__ __forceinline__ void block_sums(int64_t a, int64_t b, int64_t &before_a, int64_t &before_b, int64_t &all_a, int64_t &all_b) {
@@ -55,19 +66,24 @@ __device__ __forceinline__ uint32_t last_at_most(const uint32_t *at, uint32_t n,
     return lo;
 }
 
-// One workgroup.  Requests come in chunks of one per thread; their tokens and the pages they ask for are numbered by two prefix sums,
-// and both are then spread over all threads, which find their request by bisection.
+// Requests come in chunks of one per thread; their tokens and the pages they ask for are numbered by two prefix sums, which every
+// workgroup works out for itself, and both are then spread over all threads of the launch, which find their request by bisection.
+// The pages that tokens lie in are known from the sums, whether they are in the table yet or not; the numbers that the call
+// changes are written by the workgroup that finishes last, when nobody reads them any more.  Bound: latency (a load, two sums, a
+// bisection, a load); from some 100,000 tokens on the slots' bytes.  One workgroup for everything took 485 us for 557,000 tokens of 256 requests.
 __global__ __launch_bounds__(kTableThreads) void cache_tables_kernel(const TablesArgs a) {
     __shared__ uint32_t s_tok[kTableThreads + 1], s_page[kTableThreads + 1], s_start[kTableThreads], s_held[kTableThreads];
-    const uint32_t tid = threadIdx.x;
+    const uint32_t tid = threadIdx.x, worker = blockIdx.x * kTableThreads + tid, workers = gridDim.x * kTableThreads;
     const int32_t listed = *a.free_count;
     const uint32_t avail = listed < 0 ? 0u : (uint32_t)listed > a.free_cap ? a.free_cap : (uint32_t)listed;
     uint32_t flags = (listed < 0 || (uint32_t)listed > a.free_cap) ? kFlagBadIndex : 0u;
     int64_t tokens = 0, pages = 0;                          // of the requests before this chunk
-    for (uint32_t base = 0; base < a.nrequests; base += kTableThreads) {
-        const uint32_t r = base + tid, n = a.nrequests - base < (uint32_t)kTableThreads ? a.nrequests - base : (uint32_t)kTableThreads;
+    uint32_t start = 0, held = 0, now_held = 0;             // of this thread's request
+    // numbers the chunk's tokens and pages; leaves room for the next call
+    auto number = [&](uint32_t base, uint32_t n) {
+        const uint32_t r = base + tid;
         int64_t cnt = 0, want = 0;
-        uint32_t start = 0, held = 0;
+        start = held = 0;
         if (tid < n) {
             const int32_t s = a.start[r], c = a.count[r], h = a.held[r];
             if (s < 0 || c < 0 || h < 0 || (uint32_t)(h < 0 ? 0 : h) > a.width) flags |= kFlagBadIndex;
@@ -80,20 +96,27 @@ __global__ __launch_bounds__(kTableThreads) void cache_tables_kernel(const Table
         int64_t t0, p0, t_all, p_all;
         block_sums(cnt, want, t0, p0, t_all, p_all);
         t0 += tokens; p0 += pages;
-        const uint32_t tb = t0 < (int64_t)a.max_tokens ? (uint32_t)t0 : a.max_tokens, pb = p0 < (int64_t)avail ? (uint32_t)p0 : avail;
-        s_tok[tid] = tb; s_page[tid] = pb; s_start[tid] = start; s_held[tid] = held;
-        if (tid < n) a.token_begin[r] = (int32_t)tb;
         tokens += t_all; pages += p_all;
-        const uint32_t t_end = tokens < (int64_t)a.max_tokens ? (uint32_t)tokens : a.max_tokens;
-        const uint32_t p_end = pages < (int64_t)avail ? (uint32_t)pages : avail;
-        if (tid == n - 1) { s_tok[n] = t_end; s_page[n] = p_end; }
+        s_tok[tid] = t0 < (int64_t)a.max_tokens ? (uint32_t)t0 : a.max_tokens;
+        s_page[tid] = p0 < (int64_t)avail ? (uint32_t)p0 : avail;
+        s_start[tid] = start; s_held[tid] = held;
+        if (tid == n - 1) {
+            s_tok[n] = tokens < (int64_t)a.max_tokens ? (uint32_t)tokens : a.max_tokens;
+            s_page[n] = pages < (int64_t)avail ? (uint32_t)pages : avail;
+        }
         __syncthreads();
-        if (tid < n && s_page[tid + 1] > pb) a.held[r] = (int32_t)(held + (s_page[tid + 1] - pb));
-        for (uint32_t k = s_page[0] + tid; k < p_end; k += kTableThreads) {
+        now_held = held + (tid < n ? s_page[tid + 1] - s_page[tid] : 0u);
+    };
+    auto chunk_of = [&](uint32_t base) { return a.nrequests - base < (uint32_t)kTableThreads ? a.nrequests - base : (uint32_t)kTableThreads; };
+    for (uint32_t base = 0; base < a.nrequests; base += kTableThreads) {
+        const uint32_t n = chunk_of(base);
+        number(base, n);
+        if (blockIdx.x == 0 && tid < n) a.token_begin[base + tid] = (int32_t)s_tok[tid];
+        for (uint32_t k = s_page[0] + worker; k < s_page[n]; k += workers) {
             const uint32_t q = last_at_most(s_page, n, k);
             a.table[(uint64_t)(base + q) * a.width + s_held[q] + (k - s_page[q])] = a.free_pages[avail - 1 - k];
         }
-        for (uint32_t t = s_tok[0] + tid; t < t_end; t += kTableThreads) {
+        for (uint32_t t = s_tok[0] + worker; t < s_tok[n]; t += workers) {
             const uint32_t q = last_at_most(s_tok, n, t);
             const uint32_t pos = s_start[q] + (t - s_tok[q]), at = pos / a.page, h = s_held[q], got = s_page[q + 1] - s_page[q];
             int32_t page = -1;
@@ -104,14 +127,26 @@ __global__ __launch_bounds__(kTableThreads) void cache_tables_kernel(const Table
         }
         __syncthreads();
     }
-    if (tokens > (int64_t)a.max_tokens || pages > (int64_t)avail) flags |= kFlagOverflow;
-    const uint32_t t_end = tokens < (int64_t)a.max_tokens ? (uint32_t)tokens : a.max_tokens;
-    for (uint32_t t = t_end + tid; t < a.max_tokens; t += kTableThreads) { a.slots[t] = -1; a.positions[t] = 0; }
-    if (tid == 0) {
-        a.token_begin[a.nrequests] = (int32_t)t_end;
-        *a.free_count = (int32_t)(avail - (pages < (int64_t)avail ? (uint32_t)pages : avail));
+    const uint32_t t_end = tokens < (int64_t)a.max_tokens ? (uint32_t)tokens : a.max_tokens, taken = pages < (int64_t)avail ? (uint32_t)pages : avail;
+    for (uint32_t t = t_end + worker; t < a.max_tokens; t += workers) { a.slots[t] = -1; a.positions[t] = 0; }
+    if (blockIdx.x == 0) {
+        if (tokens > (int64_t)a.max_tokens || pages > (int64_t)avail) flags |= kFlagOverflow;
+        if (flags) atomicOr(a.flags, flags);
+        if (tid == 0) a.token_begin[a.nrequests] = (int32_t)t_end;
     }
-    if (flags) atomicOr(a.flags, flags);
+    if (!last_workgroup(a.ticket)) return;
+    if (a.nrequests <= (uint32_t)kTableThreads) {
+        if (tid < a.nrequests && now_held != held) a.held[tid] = (int32_t)now_held;
+    } else {
+        tokens = pages = 0;
+        for (uint32_t base = 0; base < a.nrequests; base += kTableThreads) {
+            const uint32_t n = chunk_of(base);
+            number(base, n);
+            if (tid < n && now_held != held) a.held[base + tid] = (int32_t)now_held;
+            __syncthreads();
+        }
+    }
+    if (tid == 0) *a.free_count = (int32_t)(avail - taken);
 }
 
 struct ReleaseArgs {
@@ -122,59 +157,62 @@ struct ReleaseArgs {
     uint32_t width;
     int32_t *free_pages, *free_count;
     uint32_t free_cap;
-    uint32_t *flags;
+    uint32_t *flags, *ticket;
 };
 
 // The surplus pages, numbered in the order in which srs_cache_tables would have handed them out, go to the end of the free list from the
 // last to the first.
 __global__ __launch_bounds__(kTableThreads) void cache_release_kernel(const ReleaseArgs a) {
     __shared__ uint32_t s_page[kTableThreads + 1], s_keep[kTableThreads];
-    const uint32_t tid = threadIdx.x;
+    const uint32_t tid = threadIdx.x, worker = blockIdx.x * kTableThreads + tid, workers = gridDim.x * kTableThreads;
     const int32_t listed = *a.free_count;
-    const uint32_t have = listed < 0 ? 0u : (uint32_t)listed > a.free_cap ? a.free_cap : (uint32_t)listed;
+    const uint32_t have = listed < 0 ? 0u : (uint32_t)listed > a.free_cap ? a.free_cap : (uint32_t)listed, room = a.free_cap - have;
     uint32_t flags = (listed < 0 || (uint32_t)listed > a.free_cap) ? kFlagBadIndex : 0u;
-    int64_t all = 0;
-    for (uint32_t base = 0; base < a.nrequests; base += kTableThreads) {       // how many there are
+    uint32_t keep = 0, extra = 0;                           // of this thread's request
+    auto look = [&](uint32_t base) {
         const uint32_t r = base + tid;
-        int64_t extra = 0;
+        keep = extra = 0;
         if (r < a.nrequests) {
             const int32_t k = a.keep[r], h = a.held[r];
             if (k < 0 || h < 0 || (uint32_t)(h < 0 ? 0 : h) > a.width) flags |= kFlagBadIndex;
-            const uint32_t keep = k < 0 ? 0u : (uint32_t)k, held = h < 0 ? 0u : (uint32_t)h > a.width ? a.width : (uint32_t)h;
+            const uint32_t held = h < 0 ? 0u : (uint32_t)h > a.width ? a.width : (uint32_t)h;
+            keep = k < 0 ? 0u : (uint32_t)k;
             extra = held > keep ? held - keep : 0;
         }
-        int64_t x, y, n, z;
+    };
+    int64_t all = 0, before = 0, x, y, n, z;
+    for (uint32_t base = 0; base < a.nrequests; base += kTableThreads) {       // how many there are
+        look(base);
         block_sums(extra, 0, x, y, n, z);
         all += n;
     }
-    const uint32_t room = a.free_cap - have;
-    if (all > (int64_t)room) flags |= kFlagOverflow;
-    int64_t before = 0;
     for (uint32_t base = 0; base < a.nrequests; base += kTableThreads) {
-        const uint32_t r = base + tid, n = a.nrequests - base < (uint32_t)kTableThreads ? a.nrequests - base : (uint32_t)kTableThreads;
-        uint32_t extra = 0, keep = 0;
-        if (tid < n) {
-            const int32_t k = a.keep[r], h = a.held[r];
-            keep = k < 0 ? 0u : (uint32_t)k;
-            const uint32_t held = h < 0 ? 0u : (uint32_t)h > a.width ? a.width : (uint32_t)h;
-            extra = held > keep ? held - keep : 0;
+        const uint32_t count = a.nrequests - base < (uint32_t)kTableThreads ? a.nrequests - base : (uint32_t)kTableThreads;
+        if (a.nrequests > (uint32_t)kTableThreads) {                            // else they are still there
+            look(base);
+            block_sums(extra, 0, x, y, n, z);
         }
-        int64_t x, y, sum, z;
-        block_sums(extra, 0, x, y, sum, z);
         s_page[tid] = (uint32_t)x; s_keep[tid] = keep;
-        if (tid == n - 1) s_page[n] = (uint32_t)sum;
+        if (tid == count - 1) s_page[count] = (uint32_t)n;
         __syncthreads();
-        for (uint32_t k = tid; k < (uint32_t)sum; k += kTableThreads) {
-            const uint32_t q = last_at_most(s_page, n, k);
+        for (uint32_t k = worker; k < (uint32_t)n; k += workers) {
+            const uint32_t q = last_at_most(s_page, count, k);
             const int64_t to = all - 1 - (before + k);                          // places behind the list's end
             if (to < (int64_t)room) a.free_pages[have + (uint32_t)to] = a.table[(uint64_t)(base + q) * a.width + s_keep[q] + (k - s_page[q])];
         }
-        if (extra) a.held[r] = (int32_t)keep;
-        before += sum;
+        before += n;
         __syncthreads();
     }
+    if (blockIdx.x == 0) {
+        if (all > (int64_t)room) flags |= kFlagOverflow;
+        if (flags) atomicOr(a.flags, flags);
+    }
+    if (!last_workgroup(a.ticket)) return;
+    for (uint32_t base = 0; base < a.nrequests; base += kTableThreads) {
+        if (a.nrequests > (uint32_t)kTableThreads) look(base);
+        if (extra) a.held[base + tid] = (int32_t)keep;
+    }
     if (tid == 0) *a.free_count = (int32_t)(have + (all < (int64_t)room ? (uint32_t)all : room));
-    if (flags) atomicOr(a.flags, flags);
 }
 
 // ---- rotary positions and rows into the cache --------------------------------------------------------------------------
@@ -277,7 +315,7 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a, bool transp
 // Rows in 16-byte pieces: a workgroup takes a token, or a share of its heads where there are few tokens.  Its sines and cosines are
 // worked out once, a thread each, while the first pieces are on their way, and serve all heads from LDS; a thread then turns
 // the two pieces that hold a run of pairs (or the one, interleaved).  Bound: memory.  One thread per pair and head, each with
-// its own sine, took twice as long: 8192 tokens of 40 heads of 128 80 us (4.2 and 2.1 TB/s, read and written).
+// its own sine, took three times as long (8192 tokens of 40 heads of 128 80 us, now 29: 5.9 TB/s read and written).
 constexpr uint32_t kTurns = 512;                            // pairs that the table holds
 
 template <class T, bool INTERLEAVED>

@@ -110,6 +110,7 @@ struct srs_plan {
 namespace {
 
 constexpr uint32_t kEpochWord = 32;         // in the allocation of the flag word; srs_status clears the first two words only
+constexpr uint32_t kTicketWord = 16;        // counter of finished workgroups of the cache's table calls, 0 between them
 
 // ticket counters sit 256 bytes apart (atomics on one cache line serialise) unless there are very
 // many buckets, which only happens with bucket sizes far below a tile
@@ -1422,6 +1423,10 @@ int srs_decode_values(srs_ctx *ctx, const uint8_t *lens, const uint8_t *low, con
 // the Rollout's key/value cache
 // ---------------------------------------------------------------------------------------------
 
+// New tokens, and pages of the free list, that a workgroup of the table calls is there for
+constexpr uint64_t kTokensEach = 2048;
+constexpr uint32_t kPagesEach = 8192;
+
 int srs_cache_tables(srs_ctx *ctx, const int32_t *start, const int32_t *count, uint32_t nrequests, uint32_t page_tokens,
                      int32_t *held, int32_t *table, uint32_t table_width, const int32_t *free_pages, int32_t *free_count,
                      uint32_t free_cap, int32_t *token_begin, int64_t *slots, int32_t *positions, uint64_t max_tokens, void *stream) {
@@ -1435,8 +1440,9 @@ int srs_cache_tables(srs_ctx *ctx, const int32_t *start, const int32_t *count, u
     hipStream_t st = (hipStream_t)stream;
     SRS_ON_DEVICE(ctx->device);
     TablesArgs a{start, count, nrequests, page_tokens, held, table, table_width, free_pages, free_count, free_cap,
-                 token_begin, slots, positions, (uint32_t)max_tokens, ctx->flags};
-    hipLaunchKernelGGL(cache_tables_kernel, dim3(1), dim3(kTableThreads), 0, st, a);
+                 token_begin, slots, positions, (uint32_t)max_tokens, ctx->flags, ctx->flags + kTicketWord};
+    const uint64_t grid = (max_tokens + kTokensEach - 1) / kTokensEach;
+    hipLaunchKernelGGL(cache_tables_kernel, dim3((uint32_t)(grid < 1 ? 1 : grid > 256 ? 256 : grid)), dim3(kTableThreads), 0, st, a);
     SRS_HIP(hipGetLastError());
     return SRS_OK;
 }
@@ -1449,8 +1455,9 @@ int srs_cache_release(srs_ctx *ctx, const int32_t *keep, uint32_t nrequests, int
     if (((uintptr_t)keep | (uintptr_t)held | (uintptr_t)table | (uintptr_t)free_pages | (uintptr_t)free_count) & 3u) return SRS_ERR_INVALID;
     hipStream_t st = (hipStream_t)stream;
     SRS_ON_DEVICE(ctx->device);
-    ReleaseArgs a{keep, nrequests, held, table, table_width, free_pages, free_count, free_cap, ctx->flags};
-    hipLaunchKernelGGL(cache_release_kernel, dim3(1), dim3(kTableThreads), 0, st, a);
+    ReleaseArgs a{keep, nrequests, held, table, table_width, free_pages, free_count, free_cap, ctx->flags, ctx->flags + kTicketWord};
+    const uint32_t grid = free_cap / kPagesEach;         // as if all that the list has room for came back
+    hipLaunchKernelGGL(cache_release_kernel, dim3(grid < 1 ? 1 : grid > 64 ? 64 : grid), dim3(kTableThreads), 0, st, a);
     SRS_HIP(hipGetLastError());
     return SRS_OK;
 }
