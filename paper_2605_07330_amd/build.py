@@ -69,7 +69,7 @@ def build_call(verbose: bool = False) -> str:
         print(f"{os.path.basename(CALL)} is not built: {', '.join(missing)} not found; single-tensor calls go through ctypes", file=sys.stderr, flush=True)
         return ""
     cmd = [cxx, "-std=c++17", "-O2", "-fPIC", "-shared", "-Wall", "-Wextra", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
-           f'-DSRS_TORCH_VERSION="{torch.__version__}"', "-isystem", python, "-isystem", include,
+           f'-DSRS_TORCH_VERSION="{torch.__version__}"', "-I", os.path.join(ROOT, "include"), "-isystem", python, "-isystem", include,
            "-isystem", os.path.join(include, "torch", "csrc", "api", "include"), CALL_SRC, "-o", CALL,
            "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
     if verbose:

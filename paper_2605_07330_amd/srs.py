@@ -138,7 +138,7 @@ def _check(rc: int, where: str) -> None:
         raise SrsError(rc, where)
 
 
-# The single-tensor calls with their checks in C++ (csrc/call.cpp): None where it is not built or was built for another torch, and each
+# The single-tensor and cache calls with their checks in C++ (csrc/call.cpp): None where it is not built or was built for another torch, and each
 # function returns None where it leaves a call to the general way below, which is the same but for the time it takes.
 try:
     from . import _call
@@ -149,7 +149,8 @@ try:
 except ImportError as e:
     warnings.warn(f"_call does not load, single-tensor calls take longer (python -m paper_2605_07330_amd.build): {e}", RuntimeWarning)
     _call = None
-_address = {n: C.cast(getattr(_lib, n), _vp).value for n in ("srs_extract", "srs_apply", "srs_extract_u8", "srs_apply_u8", "srs_extract_cast")}
+_address = {n: C.cast(getattr(_lib, n), _vp).value for n in ("srs_extract", "srs_apply", "srs_extract_u8", "srs_apply_u8", "srs_extract_cast", "srs_cache_tables",
+                                                          "srs_cache_release", "srs_rope", "srs_cache_write", "srs_cache_attention", "srs_cache_attention_workspace")}
 
 
 def _extract_native(name: str, ctx: "Context", old, new, be, I, V, counts, cap, stream, width: int, new_width: int) -> bool:
@@ -165,6 +166,16 @@ def _apply_native(name: str, ctx: "Context", weights, be, I, V, counts, cap, str
     if _call is None:
         return False
     rc = _call.apply(_address[name], ctx._h.value, weights, be, I, V, counts, cap, _stream_ptr(stream), width)
+    if rc:
+        _check(rc, name)
+    return rc is not None
+
+
+def _native(name: str, ctx: "Context", *args) -> bool:
+    """A call of the cache through its C++ function; False where that leaves it to the general way."""
+    if _call is None:
+        return False
+    rc = getattr(_call, name[4:] if name != "srs_rope" else "rope")(_address[name], ctx._h.value, ctx.device, *args)
     if rc:
         _check(rc, name)
     return rc is not None
@@ -670,6 +681,9 @@ class Context:
                      positions: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
         """Block tables, slots and positions of the new tokens of start.numel() requests; table is [requests, width], slots and
         positions are as long as the (padded) batch.  held, table, free_count and the last three are written."""
+        st = self._stream(stream)
+        if _native("srs_cache_tables", self, start, count, page_tokens, held, table, free_pages, free_count, token_begin, slots, positions, st):
+            return
         i32, n = torch.int32, start.numel()
         if table.dim() != 2 or table.shape[0] != n:
             raise TypeError(f"table: expected [{n}, width]")
@@ -681,38 +695,45 @@ class Context:
                                      self._here(free_pages, "free_pages", i32), self._here(free_count, "free_count", i32, 1),
                                      free_pages.numel(), self._here(token_begin, "token_begin", i32, n + 1),
                                      self._here(slots, "slots", torch.int64), self._here(positions, "positions", i32), slots.numel(),
-                                     self._stream(stream)), "srs_cache_tables")
+                                     st), "srs_cache_tables")
 
     def cache_release(self, keep: torch.Tensor, held: torch.Tensor, table: torch.Tensor, free_pages: torch.Tensor,
                       free_count: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
         """Requests keep their first keep[r] pages, the others go back to the free list."""
+        st = self._stream(stream)
+        if _native("srs_cache_release", self, keep, held, table, free_pages, free_count, st):
+            return
         i32, n = torch.int32, keep.numel()
         if table.dim() != 2 or table.shape[0] != n:
             raise TypeError(f"table: expected [{n}, width]")
         _check(_lib.srs_cache_release(self._h, self._here(keep, "keep", i32), n, self._here(held, "held", i32, n),
                                       self._here(table, "table", i32), table.shape[1], self._here(free_pages, "free_pages", i32),
-                                      self._here(free_count, "free_count", i32, 1), free_pages.numel(), self._stream(stream)),
-               "srs_cache_release")
+                                      self._here(free_count, "free_count", i32, 1), free_pages.numel(), st), "srs_cache_release")
 
     def rope(self, x: torch.Tensor, out: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor, interleaved: bool = False,
              magnitude: float = 1.0, transpose: bool = False, stream: Optional[torch.cuda.Stream] = None) -> None:
         """Rotary positions on x [tokens, heads, head_dim] into out (which may be x); transpose: the gradient.  inv_freq: float64."""
+        st, flags = self._stream(stream), (ROPE_INTERLEAVED if interleaved else 0) | (ROPE_TRANSPOSE if transpose else 0)
+        if _native("srs_rope", self, x, out, positions, inv_freq, flags, magnitude, st):
+            return
         if x.dim() != 3 or x.dtype not in _DTYPES:
             raise TypeError("x: expected a bfloat16, float16 or float32 tensor [tokens, heads, head_dim]")
         T, heads, d = x.shape
         if out.shape != x.shape:
             raise ValueError("x and out differ in shape")
         rx, ro = self._rows(x, "x", T, d, x.dtype), self._rows(out, "out", T, d, x.dtype)
-        flags = (ROPE_INTERLEAVED if interleaved else 0) | (ROPE_TRANSPOSE if transpose else 0)
         _check(_lib.srs_rope(self._h, _DTYPES[x.dtype], C.byref(rx), C.byref(ro), T, d, self._here(positions, "positions", torch.int32, T),
-                             self._here(inv_freq, "inv_freq", torch.float64), 2 * inv_freq.numel(), flags, magnitude,
-                             self._stream(stream)), "srs_rope")
+                             self._here(inv_freq, "inv_freq", torch.float64), 2 * inv_freq.numel(), flags, magnitude, st),
+               "srs_rope")
 
     def cache_write(self, k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, slots: torch.Tensor,
                     q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
                     inv_freq: Optional[torch.Tensor] = None, interleaved: bool = False, magnitude: float = 1.0,
                     stream: Optional[torch.cuda.Stream] = None) -> None:
         """Rows of k and v [tokens, heads, head_dim] into the cache at slots; with inv_freq k is turned on the way, and q into q_out."""
+        st, flags = self._stream(stream), ROPE_INTERLEAVED if interleaved else 0
+        if _native("srs_cache_write", self, k, v, k_cache, v_cache, slots, q, q_out, positions, inv_freq, flags, magnitude, st):
+            return
         cache = self._cache(k_cache, v_cache)
         dt, T, d = k_cache.dtype, slots.numel(), k_cache.shape[3]
         rk, rv = self._rows(k, "k", T, d, dt), self._rows(v, "v", T, d, dt)
@@ -727,7 +748,7 @@ class Context:
                 raise TypeError("q: needs q_out, positions and inv_freq")
             rq, ro = C.byref(self._rows(q, "q", T, d, dt)), C.byref(self._rows(q_out, "q_out", T, d, dt))
         _check(_lib.srs_cache_write(self._h, C.byref(cache), C.byref(rk), C.byref(rv), T, self._here(slots, "slots", torch.int64), rq, ro, pos,
-                                    freq, rot, ROPE_INTERLEAVED if interleaved else 0, magnitude, self._stream(stream)), "srs_cache_write")
+                                    freq, rot, flags, magnitude, st), "srs_cache_write")
 
     def cache_attention(self, q: torch.Tensor, out: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor,
                         token_begin: torch.Tensor, start: torch.Tensor, scale: Optional[float] = None, causal: bool = True,
@@ -736,6 +757,10 @@ class Context:
         """Attention of the new tokens q [tokens, heads, head_dim] over the paged cache.  scale: 1 / sqrt(head_dim) by default.
         most_tokens, most_keys: the most new tokens and keys of any request, as far as known.  workspace: device memory of
         attention_workspace() bytes; without it the call takes what it needs from torch, on its stream."""
+        st = self._stream(stream)
+        if _native("srs_cache_attention", self, _address["srs_cache_attention_workspace"], q, out, k_cache, v_cache, table, token_begin, start, scale,
+                   0 if causal else ATTN_FULL, window, sinks, lse, most_tokens, most_keys, workspace, st, 1 if stream is None else 0):
+            return
         cache = self._cache(k_cache, v_cache)
         T, d, n, i32 = q.shape[0], k_cache.shape[3], start.numel(), torch.int32
         rq, ro = self._rows(q, "q", T, d, k_cache.dtype), self._rows(out, "out", T, d, k_cache.dtype)
@@ -756,7 +781,7 @@ class Context:
                                         T, self._here(token_begin, "token_begin", i32, n + 1), self._here(start, "start", i32),
                                         self._here(table, "table", i32), table.shape[1], n, d ** -0.5 if scale is None else scale,
                                         0 if causal else ATTN_FULL, window, sinks, most_tokens, most_keys, ws, nbytes,
-                                        self._stream(stream)), "srs_cache_attention")
+                                        st), "srs_cache_attention")
 
     # ---- measurement aid ------------------------------------------------------------------
     def stream_probe(self, a: torch.Tensor, b: torch.Tensor, sink: torch.Tensor,
