@@ -21,7 +21,7 @@ struct AttnArgs {
     int64_t k_page, k_token, k_head, v_page, v_token, v_head;
     const int32_t *token_begin, *start, *table;
     uint32_t tokens, nrequests, width, page, pages;
-    uint32_t page_magic, page_shift;                                // j / page = j * page_magic >> page_shift for j below 2^31
+    uint32_t page_magic, page_shift;                                // j / page = j * page_magic >> 32 + page_shift for j below 2^31, unless page is 1
     uint32_t heads, kv_heads, head_dim, group;
     uint32_t window, sinks;
     float scale;                                                    // its size times log2(e); 1 where it is 0
@@ -65,9 +65,6 @@ __device__ __forceinline__ s16x4 lds_transposed(const unsigned char *p) {
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)p);
 }
 
-// the block table is read by scalar loads where a whole wave asks for the same entry
-typedef const int32_t __attribute__((address_space(4))) const_i32;
-
 template <class T> __device__ __forceinline__ T uniform_value(T x) { return (T)__builtin_amdgcn_readfirstlane((int)x); }
 
 // Values that are not finite may not meet the weights of rows that do not see them (0 hides nothing), nor weights in two parts.  They are
@@ -89,15 +86,40 @@ template <class T> __device__ __forceinline__ typename AttnTypes<T>::x8 signed_q
     return y;
 }
 
-// What the block table says about key j of a request, asked for early and looked at a key tile later, when the answer is there.
-// Nothing is asked where no row sees the key (or, with BLOCKS, any of the 16 keys that it is one of): place is then -1.
+// What the block table says about keys of a request: each lane asks for one, a tile early, and looks at the answer when it is there.
+// Nothing is asked where no row sees the key, nor, with BLOCKS, any of the 16 keys that it is the first of: place is then -1.
 struct Asked { int32_t page, place; };
-template <bool BLOCKS, class P>
-__device__ __forceinline__ Asked ask_table(const AttnArgs &a, P table, int32_t j, bool seen) {
-    const uint32_t at = (uint32_t)(((uint64_t)(uint32_t)j * a.page_magic) >> a.page_shift);
+template <bool BLOCKS>
+__device__ __forceinline__ Asked ask_table(const AttnArgs &a, const int32_t *table, int32_t j, bool seen) {
+    const uint32_t at = !BLOCKS && a.page == 1 ? (uint32_t)j : __umulhi((uint32_t)j, a.page_magic) >> a.page_shift;
     Asked x;
     x.page = table[seen ? at : 0u];
     x.place = seen ? j - (int32_t)(at * a.page) : -1;
+    return x;
+}
+
+// Where a lane's key (or block) lies behind the bases of K and V, in bytes; with BLOCKS both are the same.  Page 0 where there is none.
+struct Found { int64_t k, v; bool there, hole; };
+template <bool BLOCKS>
+__device__ __forceinline__ Found find_row(const AttnArgs &a, const Asked &x) {
+    Found f;
+    f.there = x.place >= 0 && (uint32_t)x.page < a.pages;
+    f.hole = x.place >= 0 && !f.there;
+    const int64_t page = f.there ? x.page : 0, place = x.place >= 0 ? x.place : 0;
+    f.k = (page * a.k_page + place * a.k_token) * 2;
+    f.v = BLOCKS ? f.k : (page * a.v_page + place * a.v_token) * 2;
+    return f;
+}
+__device__ __forceinline__ int64_t lane_value(int64_t x, uint32_t lane) {
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, (int)lane), hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)((uint64_t)x >> 32), (int)lane);
+    return (int64_t)(((uint64_t)hi << 32) | lo);
+}
+// Bit k: key k of a tile is there.  lanes: bit i, lane i's is.
+template <bool BLOCKS, int KEYS> __device__ __forceinline__ uint64_t there_bits(uint64_t lanes) {
+    if (!BLOCKS) return lanes;
+    uint64_t x = 0;
+#pragma unroll
+    for (int b = 0; b < KEYS / 16; ++b) x |= (lanes >> b & 1ull) * (0xffffull << (16 * b));
     return x;
 }
 
@@ -169,7 +191,7 @@ __device__ __forceinline__ void walk_values(const AttnArgs &a, const AttnTile &t
     for (int32_t k = 0; k < n; ++k) {
         const int32_t j = key + k;
         if (j >= t.end || !(j >= t.low || j < t.sinks)) continue;
-        const uint32_t at = (uint32_t)(((uint64_t)(uint32_t)j * a.page_magic) >> a.page_shift);
+        const uint32_t at = a.page == 1 ? (uint32_t)j : __umulhi((uint32_t)j, a.page_magic) >> a.page_shift;
         const int32_t page = a.table[(int64_t)t.r * a.width + at];
         if ((uint32_t)page >= a.pages) continue;
         add((const T *)a.v + (int64_t)page * a.v_page + (int64_t)(j - (int32_t)(at * a.page)) * a.v_token + (int64_t)kh * a.v_head,
@@ -274,59 +296,37 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : DP == 128 ? 2 : 1) void attenti
     const uint32_t piece = lane % kRowPieces, my_row = lane / kRowPieces;
     const bool inside = EXACT || piece * 8 < a.head_dim;
     const uint32_t piece_off = inside ? piece * 16 : 0;
-    const uint32_t k_lane = my_row * (uint32_t)a.k_token * 2 + piece_off, v_lane = my_row * (uint32_t)a.v_token * 2 + piece_off;
+    const uint32_t row_off = my_row * (uint32_t)a.k_token * 2 + piece_off;           // BLOCKS: of K and V
     const unsigned char *const k_base = a.k + (int64_t)kh * a.k_head * 2, *const v_base = a.v + (int64_t)kh * a.v_head * 2;
-    const const_i32 *const table = (const const_i32 *)(a.table + (int64_t)t.r * a.width);
-
-    // pages of the 32 keys from `key` on: of both blocks of 16 where pages hold whole blocks (scalar), else of key + lane % 32
-    constexpr int kAsk = BLOCKS ? 2 : 1;
-    struct Questions { Asked x[kAsk]; };
+    const int32_t *const table = a.table + (int64_t)t.r * a.width;
+    // of the 32 keys from `key` on: the two blocks of 16 where pages hold whole blocks, else every key
     auto ask = [&](int32_t key, bool live) {
-        Questions x;
-#pragma unroll
-        for (int b = 0; b < kAsk; ++b) {
-            const int32_t j = BLOCKS ? key + 16 * b : key + (int32_t)(lane & 31);
-            const bool seen = live & (j < t.end) & ((j + (BLOCKS ? 15 : 0) >= t.low) | (j < t.sinks));
-            if constexpr (BLOCKS) x.x[b] = ask_table<true>(a, table, j, seen);
-            else x.x[b] = ask_table<false>(a, a.table + (int64_t)t.r * a.width, j, seen);
-        }
-        return x;
-    };
-    struct Pages { int32_t page[kAsk], place[kAsk]; uint32_t ok; };                 // ok: bit k for key + k
-    auto take = [&](const Questions &x) {
-        Pages p;
-        uint32_t ok = 0;
-#pragma unroll
-        for (int b = 0; b < kAsk; ++b) {
-            const bool there = x.x[b].place >= 0 && (uint32_t)x.x[b].page < a.pages;
-            bad |= x.x[b].place >= 0 && !there;
-            p.page[b] = there ? x.x[b].page : 0;
-            p.place[b] = x.x[b].place >= 0 ? x.x[b].place : 0;
-            if constexpr (BLOCKS) ok |= there ? 0xffffu << (16 * b) : 0u;
-            else ok = (uint32_t)__ballot(there);
-        }
-        p.ok = ok;
-        return p;
+        const int32_t j = key + (int32_t)(BLOCKS ? 16 * (lane & 1) : lane & 31);
+        return ask_table<BLOCKS>(a, table, j, live & (j < t.end) & ((j + (BLOCKS ? 15 : 0) >= t.low) | (j < t.sinks)));
     };
     u32x4 kreg[kVC], vreg[kVC];
-    auto load_rows = [&](const Pages &pg, const unsigned char *base, int64_t page_stride, int64_t token_stride, uint32_t lane_off, u32x4 (&to)[kVC]) {
+    auto load_rows = [&](int64_t found, const unsigned char *base, u32x4 (&to)[kVC]) {
+        constexpr int kLoads = 16 / kRowsPerLoad;                                   // of a block
+        if constexpr (BLOCKS) {
 #pragma unroll
-        for (int c = 0; c < kVC; ++c) {
-            constexpr int kLoads = 16 / kRowsPerLoad;                               // of a block
-            if constexpr (BLOCKS) {
-                const int b = c / kLoads;
-                const auto p = scalar_base(as_global(base + ((int64_t)pg.page[b] * page_stride + ((int64_t)pg.place[b] + (c % kLoads) * kRowsPerLoad) * token_stride) * 2));
-                to[c] = __builtin_nontemporal_load((gptr<const u32x4>)(p + lane_off));
-            } else {
-                const uint32_t k = c * kRowsPerLoad + my_row;
-                const auto p = as_global(base + ((int64_t)__shfl(pg.page[0], k) * page_stride + (int64_t)__shfl(pg.place[0], k) * token_stride) * 2);
-                to[c] = __builtin_nontemporal_load((gptr<const u32x4>)(p + piece_off));
+            for (int b = 0; b < 2; ++b) {
+                const auto p = scalar_base(as_global(base + lane_value(found, b)));
+#pragma unroll
+                for (int c = 0; c < kLoads; ++c) to[b * kLoads + c] = __builtin_nontemporal_load((gptr<const u32x4>)(p + (row_off + c * (kRowsPerLoad * 2) * (uint32_t)a.k_token)));
             }
+        } else {
+#pragma unroll
+            for (int c = 0; c < kVC; ++c)
+                to[c] = __builtin_nontemporal_load((gptr<const u32x4>)as_global(base + __shfl(found, c * kRowsPerLoad + my_row) + piece_off));
         }
     };
-    auto load = [&](const Pages &pg) {
-        load_rows(pg, v_base, a.v_page, a.v_token, v_lane, vreg);
-        load_rows(pg, k_base, a.k_page, a.k_token, k_lane, kreg);
+    uint64_t ok = 0;                                                                // of the keys whose rows are in kreg and vreg
+    auto load = [&](const Asked &x) {
+        const Found f = find_row<BLOCKS>(a, x);
+        bad |= f.hole;
+        ok = there_bits<BLOCKS, 32>(__ballot(f.there));
+        load_rows(f.v, v_base, vreg);
+        load_rows(f.k, k_base, kreg);
     };
     unsigned char *const mine = s_mem + wave * kRegion, *const keys = s_keys[wave];
     auto place_of = [&](uint32_t key, uint32_t p) { return key * (DP * 2) + ((p ^ ((key & 7) << 1)) & (kRowPieces - 1)) * 16; };
@@ -338,18 +338,18 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : DP == 128 ? 2 : 1) void attenti
     bool dirty = false;
     const int32_t shift = 32 * (int32_t)wave;
     if (from < to) {
-    Pages now = take(ask(tiles.key(from, kNarrowKeys) + shift, from < to));
-    Questions next = ask(tiles.key(from + 1, kNarrowKeys) + shift, from + 1 < to);
-    load(now);
+    Asked next = ask(tiles.key(from, kNarrowKeys) + shift, true);
+    load(next);
+    next = ask(tiles.key(from + 1, kNarrowKeys) + shift, from + 1 < to);
 #pragma unroll 1
     for (int32_t i = from; i < to; ++i) {
         const int32_t key = tiles.key(i, kNarrowKeys) + shift;
         const bool more = i + 1 < to;
         // does every row see every one of these keys?
-        const bool whole = key + 32 <= all_end && (key >= all_low || key + 32 <= t.sinks) && now.ok == ~0u;
+        const bool whole = key + 32 <= all_end && (key >= all_low || key + 32 <= t.sinks) && (uint32_t)ok == ~0u;
         if (!whole) {
             // values that no row sees are 0: a weight of 0 does not hide what is not a number
-            const uint32_t any = (uint32_t)seen_bits(key, t.low, t.end, t.sinks) & now.ok;
+            const uint32_t any = (uint32_t)(seen_bits(key, t.low, t.end, t.sinks) & ok);
 #pragma unroll
             for (int c = 0; c < kVC; ++c) {
                 const bool here = any >> (c * kRowsPerLoad + my_row) & 1u;
@@ -372,10 +372,9 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : DP == 128 ? 2 : 1) void attenti
             if constexpr (EXACT) *(u32x4 *)(keys + k_place(c * kRowsPerLoad + my_row, piece)) = kreg[c];
             else *(u32x4 *)(keys + k_place(c * kRowsPerLoad + my_row, piece)) = u32x4{inside ? kreg[c][0] : 0u, inside ? kreg[c][1] : 0u, inside ? kreg[c][2] : 0u, inside ? kreg[c][3] : 0u};
         }
-        const uint32_t ok = now.ok;
-        now = take(next);
+        const uint32_t here = (uint32_t)ok;
+        if (more) load(next);
         next = ask(tiles.key(i + 2, kNarrowKeys) + shift, i + 2 < to);
-        if (more) load(now);
         float x[8], top = -INFINITY;
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
@@ -386,7 +385,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : DP == 128 ? 2 : 1) void attenti
             for (int e = 0; e < 4; ++e) x[4 * b + e] = s[e] * a.scale;
         }
         if (!whole) {
-            const uint32_t sees = ((uint32_t)seen_bits(key, row_low, row_end, t.sinks) & ok) >> (4 * g);
+            const uint32_t sees = ((uint32_t)seen_bits(key, row_low, row_end, t.sinks) & here) >> (4 * g);
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = sees >> (16 * (e >> 2) + (e & 3)) & 1u ? x[e] : -INFINITY;
         }
@@ -506,8 +505,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_wide_kernel(
     constexpr int kRowsPerLoad = 256 / kRowPieces, kRowsPerWave = kRowsPerLoad / 4, kLoads = KT / kRowsPerLoad, kBytes = KT * DP * 2;
     constexpr float kShift = AttnTypes<T>::kShift == 0.f ? 0.f : 6.f;              // with kSlack: at most 2^14 in a half
     __shared__ __attribute__((aligned(16))) unsigned char s_k[2][kBytes], s_v[2][kBytes];
-    __shared__ unsigned char s_ok[2][KT];                                          // is the key's page there
-    __shared__ int32_t s_holes[2], s_dirty;                                        // the last tile in the buffer with a key that is not; was a value not finite
+    __shared__ int32_t s_dirty;                                                    // was a value not finite
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform_value(tid >> 6), h = lane >> 5, n = lane & 31;
     const AttnShape &w = a.wide;
     uint32_t id = blockIdx.x;
@@ -554,42 +552,35 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_wide_kernel(
     const uint32_t piece = lane % kRowPieces, lane_row = lane / kRowPieces, my_row = wave * kRowsPerWave + lane_row;
     const bool inside = EXACT || piece * 8 < a.head_dim;
     const uint32_t piece_off = inside ? piece * 16 : 0;
-    const uint32_t k_lane = lane_row * (uint32_t)a.k_token * 2 + piece_off, v_lane = lane_row * (uint32_t)a.v_token * 2 + piece_off;
+    const uint32_t row_off = my_row % 16 * (uint32_t)a.k_token * 2 + piece_off;      // BLOCKS: of K and V
     const unsigned char *const k_base = a.k + (int64_t)kh * a.k_head * 2, *const v_base = a.v + (int64_t)kh * a.v_head * 2;
-    const const_i32 *const table = (const const_i32 *)(a.table + (int64_t)t.r * a.width);
-    struct Questions { Asked x[kLoads]; };
+    const int32_t *const table = a.table + (int64_t)t.r * a.width;
+    // of the tile's keys from `key` on: the blocks of 16 where pages hold whole blocks, else every key
     auto ask = [&](int32_t key, bool live) {
-        Questions x;
-#pragma unroll
-        for (int c = 0; c < kLoads; ++c) {
-            const int32_t j = key + c * kRowsPerLoad + (int32_t)(BLOCKS ? wave * kRowsPerWave : my_row), b = BLOCKS ? j & ~15 : j;
-            const bool seen = live & (b < t.end) & ((b + (BLOCKS ? 15 : 0) >= t.low) | (b < t.sinks));
-            if constexpr (BLOCKS) x.x[c] = ask_table<true>(a, table, j, seen);
-            else x.x[c] = ask_table<false>(a, a.table + (int64_t)t.r * a.width, j, seen);
-        }
-        return x;
+        const int32_t j = key + (int32_t)(BLOCKS ? 16 * (lane % (KT / 16)) : lane % KT);
+        return ask_table<BLOCKS>(a, table, j, live & (j < t.end) & ((j + (BLOCKS ? 15 : 0) >= t.low) | (j < t.sinks)));
     };
     u32x4 kst[kLoads], vst[kLoads];
-    uint32_t ok = 0;                                                               // bit c: the row that load c brought is there
+    uint64_t ok = 0;                                                               // of the keys whose rows are in kst and vst; bit i: lane i's answer
     bool hole = false;
-    auto load = [&](const Questions &x) {
-        hole = false; ok = 0;
+    auto load = [&](const Asked &x) {
+        const Found f = find_row<BLOCKS>(a, x);
+        bad |= f.hole;
+        hole = __any(f.hole);
+        ok = __ballot(f.there);
 #pragma unroll
         for (int c = 0; c < kLoads; ++c) {
-            const bool there = x.x[c].place >= 0 && (uint32_t)x.x[c].page < a.pages;
-            hole |= x.x[c].place >= 0 && !there;
-            ok |= there ? 1u << c : 0u;
-            const int64_t page = there ? x.x[c].page : 0, place = x.x[c].place >= 0 ? x.x[c].place : 0;
             if constexpr (BLOCKS) {
-                kst[c] = *(gptr<const u32x4>)(scalar_base(as_global(k_base + (page * a.k_page + place * a.k_token) * 2)) + k_lane);
-                vst[c] = *(gptr<const u32x4>)(scalar_base(as_global(v_base + (page * a.v_page + place * a.v_token) * 2)) + v_lane);
+                const int64_t at = lane_value(f.k, (c * kRowsPerLoad + wave * kRowsPerWave) / 16);
+                const uint32_t off = row_off + (kRowsPerLoad < 16 ? c * kRowsPerLoad % 16 * (uint32_t)a.k_token * 2 : 0);
+                kst[c] = *(gptr<const u32x4>)(scalar_base(as_global(k_base + at)) + off);
+                vst[c] = *(gptr<const u32x4>)(scalar_base(as_global(v_base + at)) + off);
             } else {
-                kst[c] = *(gptr<const u32x4>)as_global(k_base + (page * a.k_page + place * a.k_token) * 2 + piece_off);
-                vst[c] = *(gptr<const u32x4>)as_global(v_base + (page * a.v_page + place * a.v_token) * 2 + piece_off);
+                kst[c] = *(gptr<const u32x4>)as_global(k_base + __shfl(f.k, c * kRowsPerLoad + my_row) + piece_off);
+                vst[c] = *(gptr<const u32x4>)as_global(v_base + __shfl(f.v, c * kRowsPerLoad + my_row) + piece_off);
             }
             if constexpr (!EXACT) kst[c] = u32x4{inside ? kst[c][0] : 0u, inside ? kst[c][1] : 0u, inside ? kst[c][2] : 0u, inside ? kst[c][3] : 0u};
         }
-        bad |= hole;
     };
     auto k_place = [&](uint32_t key, uint32_t p) { return key * (DP * 2) + (p ^ (DP == 64 ? (key >> 1) & 7 : key & 15)) * 16; };
     auto v_place = [&](uint32_t key, uint32_t p) { return key * (DP * 2) + (p ^ (DP == 64 ? ((key >> 1) & 1) << 2 : (key & 3) << 2)) * 16; };
@@ -600,13 +591,12 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_wide_kernel(
     auto put = [&](int32_t i, int32_t key) {
         const int buf = i & 1;
         const bool edge = !(key + KT <= t.end && (key >= t.low || key + KT <= t.sinks));
-        const bool holes = __any(hole);
         u16x2 largest = {0, 0};
-        if (edge || holes) {                                                      // values that no row sees are 0
-            const uint64_t any = seen_bits(key, t.low, t.end, t.sinks) >> my_row;
+        if (edge || hole) {                                                       // values that no row sees are 0
+            const uint64_t any = (seen_bits(key, t.low, t.end, t.sinks) & there_bits<BLOCKS, KT>(ok)) >> my_row;
 #pragma unroll
             for (int c = 0; c < kLoads; ++c) {
-                const bool here = (any >> (c * kRowsPerLoad) & 1u) & (ok >> c & 1u);
+                const bool here = any >> (c * kRowsPerLoad) & 1u;
                 vst[c] = u32x4{here ? vst[c][0] : 0u, here ? vst[c][1] : 0u, here ? vst[c][2] : 0u, here ? vst[c][3] : 0u};
             }
         }
@@ -628,11 +618,6 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_wide_kernel(
             *(u32x4 *)(s_k[buf] + k_place(row, piece)) = kst[c];
             *(u32x4 *)(s_v[buf] + v_place(row, piece)) = vst[c];
         }
-        if (piece == 0) {
-#pragma unroll
-            for (int c = 0; c < kLoads; ++c) s_ok[buf][c * kRowsPerLoad + my_row] = (unsigned char)(ok >> c & 1u);
-        }
-        if (holes && lane == 0) s_holes[buf] = i;
     };
 
     f32x16 o[kDB];
@@ -641,10 +626,10 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_wide_kernel(
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
     float m = -INFINITY, l = 0.f;
-    if (tid < 2) { s_holes[tid] = -1; s_dirty = 0; }
+    if (tid == 0) s_dirty = 0;
     __syncthreads();
     if (from < to) {
-    Questions next = ask(tiles.key(from, KT), true);
+    Asked next = ask(tiles.key(from, KT), true);
     {
         load(next);
         next = ask(tiles.key(from + 1, KT), from + 1 < to);
@@ -657,10 +642,11 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_wide_kernel(
         const int buf = i & 1;
         const int32_t key = tiles.key(i, KT);
         const bool more = i + 1 < to;
+        const uint64_t here = ok;
+        const bool holes = hole;
         if (more) load(next);
         next = ask(tiles.key(i + 2, KT), i + 2 < to);
         if (key < any_end && (key + KT > any_low || key < t.sinks)) {              // some row of the wave sees something
-            const bool holes = uniform_value(s_holes[buf]) == i;
             const bool whole = key + KT <= all_end && (key >= all_low || key + KT <= t.sinks) && !holes;
             float x[kB][16], top = -INFINITY;
 #pragma unroll
@@ -675,7 +661,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_wide_kernel(
             }
             if (!whole) {
                 uint64_t sees = seen_bits(key, row_low, row_end, t.sinks);
-                if (holes) sees &= __ballot(s_ok[buf][lane % KT] != 0);
+                if (holes) sees &= there_bits<BLOCKS, KT>(here);
                 const uint64_t mine = sees >> (4 * h);
 #pragma unroll
                 for (int b = 0; b < kB; ++b)

@@ -761,10 +761,10 @@ void attention_parts(AttnShape &w, uint32_t q_heads, uint32_t head_dim, float *&
     at += cells * (head_dim + 4);
 }
 
-// Pages that hold whole blocks of 16 keys, whose rows a 32-bit offset spans: addresses are then scalar but for that offset.
+// Pages that hold whole blocks of 16 keys, alike for keys and values, whose rows a 32-bit offset spans: a block is looked up once, its address
+// is scalar and serves both.
 bool in_blocks(const srs_cache *c) {
-    const int64_t most = 1ll << 26;
-    return c->page_tokens % 16 == 0 && c->k_token >= 0 && c->k_token <= most && c->v_token >= 0 && c->v_token <= most;
+    return c->page_tokens % 16 == 0 && c->k_page == c->v_page && c->k_token == c->v_token && c->k_token >= 0 && c->k_token <= 1ll << 26;
 }
 
 template <class T, int DP>
@@ -1547,9 +1547,9 @@ int srs_cache_attention(srs_ctx *ctx, const srs_cache *cache, const srs_rows *q,
     a.v_page = cache->v_page; a.v_token = cache->v_token; a.v_head = cache->v_head;
     a.token_begin = token_begin; a.start = start; a.table = table;
     a.tokens = (uint32_t)tokens; a.nrequests = nrequests; a.width = table_width; a.page = cache->page_tokens; a.pages = cache->pages;
-    uint32_t log = 0;                                   // ceil(log2(page)): the quotient is exact for numerators below 2^31
+    uint32_t log = 0;                                   // ceil(log2(page)): the quotient is exact for numerators below 2^31; a page of 1 takes none
     while ((1ull << log) < cache->page_tokens) ++log;
-    a.page_magic = (uint32_t)(((1ull << (31 + log)) + cache->page_tokens - 1) / cache->page_tokens); a.page_shift = 31 + log;
+    a.page_magic = (uint32_t)(((1ull << (31 + log)) + cache->page_tokens - 1) / cache->page_tokens); a.page_shift = log ? log - 1 : 0;
     a.heads = q->heads; a.kv_heads = cache->heads; a.head_dim = cache->head_dim; a.group = q->heads / cache->heads;
     a.window = window; a.sinks = sinks; a.full = (flags & SRS_ATTN_FULL) != 0; a.flags = ctx->flags;
     a.scale = scale == 0.f ? 1.f : std::fabs(scale) * 1.44269504088896340736f;
