@@ -229,7 +229,7 @@ __device__ __forceinline__ uint32_t parts_of(const AttnShape &w, int32_t all) {
 }
 
 // ---- few rows: decoding ------------------------------------------------------------------------------------------------------
-// 16 rows to a workgroup, 32 keys of a tile of 128 to each of its four waves, which join their results at the end.  Scores come as
+// 16 rows to a workgroup, 32 keys of a tile to each of its four or eight waves, which join their results at the end.  Scores come as
 // K Q^T (keys down, rows across: v_mfma 16x16x32), so that a lane holds the weights of one row for eight keys, which is how the second
 // product V^T P^T takes them if its keys are counted in the same order.  K and V pass through LDS, wave by wave: V for its transposed
 // read, K so that memory is read by whole rows, past the caches (128 requests of up to 8192 keys: 464 us with K straight from
@@ -237,16 +237,15 @@ __device__ __forceinline__ uint32_t parts_of(const AttnShape &w, int32_t all) {
 // in each row so that neither read meets itself on a bank.  The next tile's rows are in flight meanwhile.
 // Bound: the cache's bytes.  Weights meet the values in two parts (value and remainder of its rounding): the second product costs
 // nothing here.
-constexpr int kNarrowKeys = 128;
-
-template <class T, int DP, bool BLOCKS, bool EXACT>
-__global__ __launch_bounds__(256, DP == 64 ? 3 : DP == 128 ? 2 : 1) void attention_narrow_kernel(const AttnArgs a) {
+template <class T, int DP, bool BLOCKS, bool EXACT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, DP == 64 ? 3 : DP == 128 ? 2 : 1) void attention_narrow_kernel(const AttnArgs a) {
+    constexpr int kNarrowKeys = 32 * WAVES;
     typedef typename AttnTypes<T>::x8 x8;
     typedef typename AttnTypes<T>::x4 x4;
     constexpr int kQC = DP / 32, kVC = DP / 16, kRegion = 64 * DP + 256, kRowPieces = DP / 8;      // 32 rows of V, or 16 of float results; pieces of 16 bytes
-    __shared__ __attribute__((aligned(16))) unsigned char s_mem[4 * kRegion];
-    __shared__ __attribute__((aligned(16))) unsigned char s_keys[4][64 * DP];
-    __shared__ float s_m[4][16], s_l[4][16];
+    __shared__ __attribute__((aligned(16))) unsigned char s_mem[WAVES * kRegion];
+    __shared__ __attribute__((aligned(16))) unsigned char s_keys[WAVES][64 * DP];
+    __shared__ float s_m[WAVES][16], s_l[WAVES][16];
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform_value(tid >> 6), g = lane >> 4, n = lane & 15;
     const AttnShape &w = a.narrow;
     uint32_t id = blockIdx.x;
@@ -432,7 +431,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : DP == 128 ? 2 : 1) void attenti
     }
     if (bad) atomicOr(a.flags, kFlagBadIndex);
 
-    // the four waves' results, in each wave's own region
+    // the waves' results, in each wave's own region
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
     float *const os = (float *)mine;
@@ -441,13 +440,13 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : DP == 128 ? 2 : 1) void attenti
     if (lane < 16) { s_m[wave][lane] = m; s_l[wave][lane] = l; }
     __syncthreads();
     const uint32_t orow = tid >> 4, otoken = orow / w.block, ohead = block * w.block + orow % w.block;
-    if (t.i0 + (int32_t)otoken >= t.i1 || ohead >= a.group || otoken >= w.tile_tokens) continue;
-    float M = -INFINITY, L = 0.f, share[4];
+    if (t.i0 + (int32_t)otoken >= t.i1 || ohead >= a.group || otoken >= w.tile_tokens || tid >= 256) continue;
+    float M = -INFINITY, L = 0.f, share[WAVES];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) M = fmaxf(M, s_m[k][orow]);
+    for (int k = 0; k < WAVES; ++k) M = fmaxf(M, s_m[k][orow]);
     const float base = M == -INFINITY ? 0.f : M;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) { share[k] = __builtin_amdgcn_exp2f(s_m[k][orow] - base); L += share[k] * s_l[k][orow]; }
+    for (int k = 0; k < WAVES; ++k) { share[k] = __builtin_amdgcn_exp2f(s_m[k][orow] - base); L += share[k] * s_l[k][orow]; }
     const bool some = !(M == -INFINITY && L == 0.f);
     const float inv = some ? 1.f / L : 0.f;
     const uint64_t out_row = (uint64_t)(t.first_row + t.i0) + otoken;
@@ -459,7 +458,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : DP == 128 ? 2 : 1) void attenti
         if (d >= a.head_dim) continue;
         float y[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < WAVES; ++k) {
             const f32x4 part = *(const f32x4 *)((const float *)(s_mem + k * kRegion) + orow * (DP + 4) + d);
 #pragma unroll
             for (int e = 0; e < 4; ++e) y[e] += share[k] * part[e];
@@ -751,6 +750,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_wide_kernel(
     }
 }
 
+constexpr int kSplitKeys = 128;                             // keys of a tile of the narrow kernel where they are shared out: four waves
+
 // ---- joining the parts -------------------------------------------------------------------------------------------------------
 // A workgroup per row and head whose keys were shared out: the parts' results weighted by exp2 of their lse.  Eight parts are read at
 // once (32 threads take four elements each of one, four parts in flight each), so that hundreds of parts cost a few round trips.
@@ -775,7 +776,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttnArgs a) {
     }
     if (i >= (uint32_t)t.n) return;
     open_tile(a, (int32_t)(i / w.tile_tokens * w.tile_tokens), w.tile_tokens, t);
-    const uint32_t n = parts_of(w, KeyTiles(t, WIDE ? (a.head_dim <= 128 ? 64 : 32) : kNarrowKeys).all);
+    const uint32_t n = parts_of(w, KeyTiles(t, WIDE ? (a.head_dim <= 128 ? 64 : 32) : kSplitKeys).all);
     if (n <= 1) return;
     const uint64_t row = (uint64_t)t.first_row + i, stride = w.slots * a.heads;
     const float *const lse = w.part_lse + cell, *const part = w.part_o + cell * a.head_dim;

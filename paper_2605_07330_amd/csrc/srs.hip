@@ -697,6 +697,7 @@ constexpr uint64_t kMaxKeys = 1ull << 30;              // of one request
 struct AttnPlan {
     AttnShape narrow, wide;
     uint32_t narrow_most, split_tokens, wide_tiles;
+    bool eight;                         // waves of the narrow kernel, instead of four
     uint64_t workspace;
 };
 
@@ -706,6 +707,13 @@ struct AttnPlan {
 // full without (528 workgroups of 35 key tiles in two parts 166 us and 109 to join).  And the fewest key tiles worth a workgroup.
 constexpr uint64_t kNarrowWorkgroups = 3072, kWideWorkgroups = 512;
 constexpr uint64_t kLeastNarrowTiles = 2, kLeastWideTiles = 4;
+
+// Where the narrow kernel would share keys out, its workgroups may have eight waves and go through all of them instead, which saves joining
+// parts: for up to kEightTiles key tiles, and, where there are tiles enough for most CUs, up to kEightWork over all of them.
+// Four waves and parts / eight, us (heads of 128, requests times key heads, longest context, the shortest an eighth of it): 32 of 500 keys 12.2 / 10.6, of 1000
+// 12.3 / 15.2, 128 of 1000 17.3 / 18.3, 256 of 500 17.6 / 13.0, of 1000 29.4 / 21.1, of 4000 65.8 / 65.7, 512 of 2000 71.3 / 63.8, of
+// 4000 116.1 / 114.7, 1024 of 500 54.8 / 50.2, of 1000 73.3 / 72.3, of 2000 116.3 / 120.5.
+constexpr uint64_t kEightTiles = 4, kEightUnits = 192, kEightWork = 8192;
 
 void attention_shape(AttnShape &w, uint32_t rows, uint32_t group, uint32_t key_step, uint64_t keys, uint32_t window, uint32_t sinks,
                      uint64_t tiles, uint32_t kv_heads, uint64_t workgroups, uint64_t least) {
@@ -732,7 +740,10 @@ AttnPlan attention_plan(uint32_t nrequests, uint64_t tokens, uint32_t q_heads, u
     uint64_t keys = (uint64_t)table_width * page_tokens;
     if (most_keys && most_keys < keys) keys = most_keys;
     const uint64_t busy = tokens < nrequests ? tokens : nrequests;
-    attention_shape(p.narrow, 16, group, kNarrowKeys, keys, window, sinks, busy, kv_heads, kNarrowWorkgroups, kLeastNarrowTiles);
+    attention_shape(p.narrow, 16, group, kSplitKeys, keys, window, sinks, busy, kv_heads, kNarrowWorkgroups, kLeastNarrowTiles);
+    const uint64_t units = busy * kv_heads * p.narrow.head_blocks, key_tiles = (uint64_t)p.narrow.splits * p.narrow.split_tiles;
+    p.eight = p.narrow.splits > 1 && head_dim <= 128 && (key_tiles <= kEightTiles || (units >= kEightUnits && units * key_tiles <= kEightWork));
+    if (p.eight) { p.narrow.splits = 1; p.narrow.split_tiles = 0x7fffffff; }
     // A request whose new tokens fit one narrow tile is read once by it; the wide kernel takes the others, unless there are none.
     const bool only_narrow = most_tokens && most_tokens <= p.narrow.tile_tokens;
     p.narrow_most = only_narrow ? 0x7fffffffu : p.narrow.tile_tokens;
@@ -768,7 +779,7 @@ bool in_blocks(const srs_cache *c) {
 }
 
 template <class T, int DP>
-int launch_attention(const AttnArgs &a, bool blocks, hipStream_t st) {
+int launch_attention(const AttnArgs &a, bool blocks, bool eight, hipStream_t st) {
     const dim3 narrow(a.nrequests * a.narrow.splits * a.kv_heads * a.narrow.head_blocks), wide(a.wide_tiles * a.wide.splits * a.kv_heads * a.wide.head_blocks);
 #define SRS_ATTENTION(BLOCKS, EXACT)                                                                                    \
     do {                                                                                                                \
@@ -776,7 +787,10 @@ int launch_attention(const AttnArgs &a, bool blocks, hipStream_t st) {
             hipLaunchKernelGGL((attention_wide_kernel<T, DP, BLOCKS, EXACT>), wide, dim3(256), 0, st, a);               \
             SRS_HIP(hipGetLastError());                                                                                 \
         }                                                                                                               \
-        hipLaunchKernelGGL((attention_narrow_kernel<T, DP, BLOCKS, EXACT>), narrow, dim3(256), 0, st, a);               \
+        if constexpr (DP <= 128) {                                                                                      \
+            if (eight) hipLaunchKernelGGL((attention_narrow_kernel<T, DP, BLOCKS, EXACT, 8>), narrow, dim3(512), 0, st, a); \
+        }                                                                                                               \
+        if (!eight) hipLaunchKernelGGL((attention_narrow_kernel<T, DP, BLOCKS, EXACT, 4>), narrow, dim3(256), 0, st, a); \
         SRS_HIP(hipGetLastError());                                                                                     \
     } while (0)
     if (blocks && a.head_dim == DP) SRS_ATTENTION(true, true);
@@ -795,10 +809,10 @@ int launch_attention(const AttnArgs &a, bool blocks, hipStream_t st) {
 }
 
 template <class T>
-int launch_attention(const AttnArgs &a, bool blocks, hipStream_t st) {
-    if (a.head_dim <= 64) return launch_attention<T, 64>(a, blocks, st);
-    if (a.head_dim <= 128) return launch_attention<T, 128>(a, blocks, st);
-    return launch_attention<T, 256>(a, blocks, st);
+int launch_attention(const AttnArgs &a, bool blocks, bool eight, hipStream_t st) {
+    if (a.head_dim <= 64) return launch_attention<T, 64>(a, blocks, eight, st);
+    if (a.head_dim <= 128) return launch_attention<T, 128>(a, blocks, eight, st);
+    return launch_attention<T, 256>(a, blocks, eight, st);
 }
 }  // namespace
 
@@ -1559,8 +1573,8 @@ int srs_cache_attention(srs_ctx *ctx, const srs_cache *cache, const srs_rows *q,
     attention_parts(a.narrow, q->heads, cache->head_dim, at);
     attention_parts(a.wide, q->heads, cache->head_dim, at);
     const bool blocks = in_blocks(cache);
-    if (cache->dtype == SRS_BF16) return launch_attention<__bf16>(a, blocks, st);
-    return launch_attention<_Float16>(a, blocks, st);
+    if (cache->dtype == SRS_BF16) return launch_attention<__bf16>(a, blocks, p.eight, st);
+    return launch_attention<_Float16>(a, blocks, p.eight, st);
 }
 
 // ---------------------------------------------------------------------------------------------
