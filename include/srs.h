@@ -413,7 +413,8 @@ typedef struct {
  * SRS_ROPE_TRANSPOSE turns by -a: with the same magnitude it takes the gradient of out to that of x.  inv_freq[rot_dim / 2] and the
  * magnitude carry whatever scaling for long contexts the model has.  The angle is taken in double, as far positions need; sine,
  * cosine and the products are binary32, rounded once to the element type (nearest, ties to even).
- * Any strides, alignment and head sizes; out may be x with the same strides, and otherwise overlaps nothing.
+ * Any strides, alignment and head sizes (rows in 16-byte pieces are several times faster); out may be x with the same strides, and
+ * otherwise overlaps nothing.  A call takes below 2^24 tokens.
  */
 #define SRS_ROPE_INTERLEAVED 1u
 #define SRS_ROPE_TRANSPOSE   2u
@@ -425,7 +426,7 @@ int srs_rope(srs_ctx *ctx, int dtype, const srs_rows *x, const srs_rows *out, ui
  * outside the cache is left out and raises SRS_FLAG_BAD_INDEX, a slot that comes twice is a caller error (one of the rows wins).  With
  * rot_dim > 0 keys are turned as in srs_rope on the way (positions, inv_freq, flags, magnitude as there), and where q is given q_out
  * receives the turned queries of every row, whatever its slot; with rot_dim = 0 positions, inv_freq, q and q_out are not used.
- * q_out may be q with the same strides.  Any strides and alignment.
+ * q_out may be q with the same strides.  Any strides and alignment.  A call takes below 2^24 tokens.
  */
 int srs_cache_write(srs_ctx *ctx, const srs_cache *cache, const srs_rows *k, const srs_rows *v, uint64_t tokens,
                     const int64_t *slots, const srs_rows *q, const srs_rows *q_out, const int32_t *positions, const double *inv_freq,
@@ -436,9 +437,12 @@ int srs_cache_write(srs_ctx *ctx, const srs_cache *cache, const srs_rows *k, con
  * are the first start[r] + count tokens of its row of table (count = its number of rows; the new tokens' own keys are in the cache
  * already).  The row at position p = start[r] + i sees the keys j <= p, with window > 0 of them those with p - j < window or j < sinks:
  *     s_j = scale * q . k_j,   out = sum_j exp(s_j) v_j / sum_j exp(s_j),   lse = log sum_j exp(s_j)
- * Query head h reads key head h / (q->heads / cache->heads).  With SRS_ATTN_FULL every row sees all start[r] + count keys (window and sinks 0).  A row that sees no key is 0, its lse -inf.  Hidden keys and values do not enter,
- * whatever their bits are.  Rows outside every request are left as they are.  Sums, maxima and products are binary32; the weights
- * exp(s_j) are rounded to the element type before they meet the values unless a kernel carries them in two parts; out is rounded once.
+ * Query head h reads key head h / (q->heads / cache->heads).  With SRS_ATTN_FULL every row sees all start[r] + count keys (window and sinks 0;
+ * sinks need a window).  A row that sees no key is 0, its lse -inf.  Hidden keys and values do not enter, whatever their bits are.  Rows
+ * outside every request are left as they are.  out may be q with the same strides, and otherwise overlaps nothing.
+ * Sums, maxima and products are binary32, and out is rounded once.  Where a request has few new tokens (those of 16 / (q->heads /
+ * cache->heads), at least one) the weights exp(s_j) meet the values in two parts of the element type, otherwise rounded to it; weights
+ * below 2^-126 of a row's largest are 0.  The same call gives the same bits each time.
  * q, out and cache are BF16 or FP16; head_dim a multiple of 8 up to 256; q->heads a multiple of cache->heads; every pointer 16-byte
  * aligned and every stride a multiple of 8 elements.  lse (tokens x q->heads, contiguous) may be NULL.  A page outside the cache that a
  * row would read counts as hidden and raises SRS_FLAG_BAD_INDEX, as does a request whose rows lie outside 0 .. tokens (it is left out).  Keys

@@ -753,15 +753,20 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_wide_kernel(
 constexpr int kSplitKeys = 128;                             // keys of a tile of the narrow kernel where they are shared out: four waves
 
 // ---- joining the parts -------------------------------------------------------------------------------------------------------
-// A workgroup per row and head whose keys were shared out: the parts' results weighted by exp2 of their lse.  Eight parts are read at
-// once (32 threads take four elements each of one, four parts in flight each), so that hundreds of parts cost a few round trips.
-template <class T, bool WIDE>
-__global__ __launch_bounds__(256) void attention_join_kernel(const AttnArgs a) {
-    __shared__ float s_top[4], s_sum[8];
-    __shared__ f32x4 s_o[8][64];
-    const uint32_t tid = threadIdx.x, lane = tid & 63;
+// The parts' results of a row and head weighted by exp2 of their lse; 32 threads take four elements each (eight above 128) of a part.  Few
+// parts: a wave to a row and head, two parts at once.  Many: a workgroup of 32 such groups, so that hundreds of parts cost a few round trips
+// (171 parts: 17 us with 8 groups, 11 with 32).
+constexpr uint32_t kFewParts = 8;
+
+template <class T, bool WIDE, bool MANY>
+__global__ __launch_bounds__(MANY ? 1024 : 256) void attention_join_kernel(const AttnArgs a) {
+    constexpr int kWaves = MANY ? 16 : 1;
+    __shared__ float s_top[kWaves], s_sum[kWaves];
+    __shared__ f32x4 s_o[kWaves][MANY ? 64 : 1];
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform_value(tid >> 6);
     const AttnShape &w = WIDE ? a.wide : a.narrow;
-    const uint64_t cell = blockIdx.x;
+    const uint64_t cell = MANY ? blockIdx.x : (uint64_t)blockIdx.x * 4 + wave;
+    if (cell >= w.slots * a.heads) return;
     const uint32_t slot = (uint32_t)(cell / a.heads), head = (uint32_t)(cell % a.heads);
     // the row's tile, and how many parts its keys came in
     AttnTile t;
@@ -781,41 +786,51 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttnArgs a) {
     const uint64_t row = (uint64_t)t.first_row + i, stride = w.slots * a.heads;
     const float *const lse = w.part_lse + cell, *const part = w.part_o + cell * a.head_dim;
     float M = -INFINITY;
-    for (uint32_t s = tid; s < n; s += 256) M = fmaxf(M, lse[s * stride]);
+    for (uint32_t s = MANY ? tid : lane; s < n; s += 64 * kWaves) M = fmaxf(M, lse[s * stride]);
 #pragma unroll
     for (int x = 1; x < 64; x *= 2) M = fmaxf(M, __shfl_xor(M, x));
-    if (lane == 0) s_top[tid >> 6] = M;
-    __syncthreads();
-    M = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
+    if constexpr (MANY) {
+        if (lane == 0) s_top[wave] = M;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kWaves; ++k) M = fmaxf(M, s_top[k]);
+    }
     const float base = M == -INFINITY ? 0.f : M;
-    const uint32_t group = tid >> 5, piece = tid & 31;                             // head_dim / 4 pieces, two to a thread above 128
+    const uint32_t group = (MANY ? tid : lane) >> 5, piece = lane & 31;
     float L = 0.f;
     f32x4 o[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll 4
-    for (uint32_t s = group; s < n; s += 8) {
+    for (uint32_t s = group; s < n; s += 2 * kWaves) {
         const float share = __builtin_amdgcn_exp2f(lse[s * stride] - base);
         L += share;
         const float *p = part + s * stride * a.head_dim;
         if (piece * 4 < a.head_dim) o[0] += share * *(const f32x4 *)(p + piece * 4);
         if (piece * 4 + 128 < a.head_dim) o[1] += share * *(const f32x4 *)(p + piece * 4 + 128);
     }
-    s_o[group][piece] = o[0]; s_o[group][piece + 32] = o[1];
-    if (piece == 0) s_sum[group] = L;
-    __syncthreads();
-    L = 0.f;
+    L += __shfl_xor(L, 32);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) L += s_sum[k];
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[k][e] += __shfl_xor(o[k][e], 32);
+    f32x4 x = lane < 32 ? o[0] : o[1];                                              // lane: elements 4 * lane on
+    if constexpr (MANY) {
+        s_o[wave][lane] = x;
+        if (lane == 0) s_sum[wave] = L;
+        __syncthreads();
+        if (wave) return;
+        L = 0.f;
+        x = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < kWaves; ++k) { L += s_sum[k]; x += s_o[k][lane]; }
+    }
     const bool some = !(M == -INFINITY && L == 0.f);
-    if (tid < 64 && tid * 4 < a.head_dim) {
-        f32x4 x = s_o[0][tid];
-#pragma unroll
-        for (int k = 1; k < 8; ++k) x += s_o[k][tid];
+    if (lane * 4 < a.head_dim) {
         const float inv = some ? 1.f / L : 0.f;
         typedef typename AttnTypes<T>::x4 x4;
-        *(x4 *)((T *)a.out + (int64_t)row * a.o_token + (int64_t)head * a.o_head + tid * 4) =
+        *(x4 *)((T *)a.out + (int64_t)row * a.o_token + (int64_t)head * a.o_head + lane * 4) =
             x4{(T)(some ? x[0] * inv : 0.f), (T)(some ? x[1] * inv : 0.f), (T)(some ? x[2] * inv : 0.f), (T)(some ? x[3] * inv : 0.f)};
     }
-    if (tid == 0 && a.lse) a.lse[row * a.heads + head] = some ? (base + __builtin_amdgcn_logf(L)) * 0.69314718055994530942f : -INFINITY;
+    if (lane == 0 && a.lse) a.lse[row * a.heads + head] = some ? (base + __builtin_amdgcn_logf(L)) * 0.69314718055994530942f : -INFINITY;
 }
 
 }  // namespace srs

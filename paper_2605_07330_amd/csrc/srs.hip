@@ -630,6 +630,9 @@ uint32_t elem_bytes(int dtype) { return dtype == SRS_BF16 || dtype == SRS_FP16 ?
 
 bool stride_ok(int64_t s) { return s >= -(1ll << 40) && s <= (1ll << 40); }
 
+// A launch has below 2^32 threads.
+bool grid_ok(uint64_t workgroups, uint32_t threads) { return workgroups * threads <= 0xffffffffull; }
+
 // Pointer and strides of rows of `tokens` tokens; `align` in bytes.
 bool rows_ok(const srs_rows *r, uint32_t align) {
     return r && r->p && r->heads > 0 && r->heads <= 65536 && ((uintptr_t)r->p & (align - 1)) == 0 && stride_ok(r->token_stride) && stride_ok(r->head_stride);
@@ -639,6 +642,8 @@ bool cache_ok(const srs_cache *c, uint32_t align) {
     if (!c || (c->pages && (!c->k || !c->v)) || !elem_bytes(c->dtype) || c->page_tokens == 0 || c->heads == 0 || c->heads > 65536 || c->head_dim == 0 || c->head_dim > 65536)
         return false;
     if (c->pages > kMaxIndexable || c->page_tokens > kMaxIndexable || (((uintptr_t)c->k | (uintptr_t)c->v) & (align - 1))) return false;
+    const auto within = [](uint64_t n, int64_t stride) { return n == 0 || (uint64_t)(stride < 0 ? -stride : stride) <= kMaxSlots / n; };
+    if (!within(c->pages, c->k_page) || !within(c->pages, c->v_page) || !within(c->page_tokens, c->k_token) || !within(c->page_tokens, c->v_token)) return false;
     return stride_ok(c->k_page) && stride_ok(c->k_token) && stride_ok(c->k_head) && stride_ok(c->v_page) && stride_ok(c->v_token) && stride_ok(c->v_head);
 }
 
@@ -672,7 +677,7 @@ int launch_rope(RopeArgs &a, int dtype, uint32_t flags, hipStream_t st) {
     const uint64_t most = (heads * each + 255) / 256, wanted = (1024 + a.tokens - 1) / a.tokens;
     a.shares = (uint32_t)(most < wanted ? most : wanted);
     const uint64_t blocks = (uint64_t)a.tokens * a.shares;
-    if (blocks > 0x7fffffffull) return SRS_ERR_INVALID;
+    if (!grid_ok(blocks, 256)) return SRS_ERR_INVALID;
 #define SRS_ROPE_LAUNCH(T)                                                                                                      \
     do {                                                                                                                        \
         const dim3 grid((uint32_t)blocks);                                                                                      \
@@ -778,6 +783,16 @@ bool in_blocks(const srs_cache *c) {
     return c->page_tokens % 16 == 0 && c->k_page == c->v_page && c->k_token == c->v_token && c->k_token >= 0 && c->k_token <= 1ll << 26;
 }
 
+template <class T, bool WIDE>
+int launch_join(const AttnArgs &a, const AttnShape &w, hipStream_t st) {
+    if (w.splits <= 1) return SRS_OK;
+    const uint64_t cells = w.slots * a.heads;
+    if (w.splits <= kFewParts) hipLaunchKernelGGL((attention_join_kernel<T, WIDE, false>), dim3((uint32_t)((cells + 3) / 4)), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((attention_join_kernel<T, WIDE, true>), dim3((uint32_t)cells), dim3(1024), 0, st, a);
+    SRS_HIP(hipGetLastError());
+    return SRS_OK;
+}
+
 template <class T, int DP>
 int launch_attention(const AttnArgs &a, bool blocks, bool eight, hipStream_t st) {
     const dim3 narrow(a.nrequests * a.narrow.splits * a.kv_heads * a.narrow.head_blocks), wide(a.wide_tiles * a.wide.splits * a.kv_heads * a.wide.head_blocks);
@@ -797,15 +812,9 @@ int launch_attention(const AttnArgs &a, bool blocks, bool eight, hipStream_t st)
     else if (blocks) SRS_ATTENTION(true, false);
     else SRS_ATTENTION(false, false);
 #undef SRS_ATTENTION
-    if (a.narrow.splits > 1) {
-        hipLaunchKernelGGL((attention_join_kernel<T, false>), dim3((uint32_t)(a.narrow.slots * a.heads)), dim3(256), 0, st, a);
-        SRS_HIP(hipGetLastError());
-    }
-    if (a.wide.splits > 1) {
-        hipLaunchKernelGGL((attention_join_kernel<T, true>), dim3((uint32_t)(a.wide.slots * a.heads)), dim3(256), 0, st, a);
-        SRS_HIP(hipGetLastError());
-    }
-    return SRS_OK;
+    int rc = launch_join<T, false>(a, a.narrow, st);
+    if (rc == SRS_OK) rc = launch_join<T, true>(a, a.wide, st);
+    return rc;
 }
 
 template <class T>
@@ -1547,8 +1556,10 @@ int srs_cache_attention(srs_ctx *ctx, const srs_cache *cache, const srs_rows *q,
     const AttnPlan p = attention_plan(nrequests, tokens, q->heads, cache->heads, cache->head_dim, table_width, cache->page_tokens, window, sinks,
                                       most_tokens, most_keys);
     if (p.workspace && (!workspace || ((uintptr_t)workspace & 15u) || workspace_bytes < p.workspace)) return SRS_ERR_INVALID;
-    if ((uint64_t)nrequests * p.narrow.splits * cache->heads * p.narrow.head_blocks > 0x7fffffffull || p.narrow.slots * q->heads > 0x7fffffffull ||
-        (uint64_t)p.wide_tiles * p.wide.splits * cache->heads * p.wide.head_blocks > 0x7fffffffull || tokens * q->heads > 0x7fffffffull)
+    if (!grid_ok((uint64_t)nrequests * p.narrow.splits * cache->heads * p.narrow.head_blocks, p.eight ? 512 : 256) ||
+        !grid_ok((uint64_t)p.wide_tiles * p.wide.splits * cache->heads * p.wide.head_blocks, 256) || tokens * q->heads > 0x7fffffffull ||
+        (p.narrow.splits > 1 && !grid_ok(p.narrow.slots * q->heads, p.narrow.splits <= kFewParts ? 64 : 1024)) ||
+        (p.wide.splits > 1 && !grid_ok(p.wide.slots * q->heads, p.wide.splits <= kFewParts ? 64 : 1024)))
         return SRS_ERR_INVALID;
     hipStream_t st = (hipStream_t)stream;
     SRS_ON_DEVICE(ctx->device);

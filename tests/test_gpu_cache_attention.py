@@ -352,6 +352,40 @@ def test_without_lse_and_the_same_again(ctx):
         assert torch.equal(out, again)                                  # and bit for bit the same each time
 
 
+@pytest.mark.parametrize("count", [[1, 1, 1], [3, 1, 90]])
+def test_in_place(ctx, count):
+    """The output over the queries."""
+    b = Batch([37, 4000, 777], count, 8, 2, 128, 16)
+    want = b.expect()
+    compare(b.call(ctx, out=b.q), want)
+    assert ctx.status() == 0
+
+
+@pytest.mark.parametrize("count", [1, 40])
+def test_keys_and_values_laid_out_differently(ctx, count):
+    b = Batch([500, 70], [count, 1], 8, 2, 128, 16)
+    b.v = b.v.transpose(1, 2).contiguous().transpose(1, 2)
+    check(ctx, b)
+    b.k = torch.cat([b.k, b.k], 3)[..., 128:]                           # wider rows
+    check(ctx, b)
+
+
+def test_many_requests(ctx):
+    """More than one round of the search for a row's request; requests without rows among them."""
+    g = torch.Generator().manual_seed(4)
+    start, count = torch.randint(0, 60, (700,), generator=g).tolist(), torch.randint(0, 3, (700,), generator=g).tolist()
+    count[5], count[350], count[699] = 40, 33, 21
+    check(ctx, Batch(start, count, 2, 1, 64, 16))
+
+
+def test_parts_of_many_requests(ctx):
+    """Few parts each, of some only; heads that share a key head in two blocks."""
+    start = [50] * 69 + [5000]
+    check(ctx, Batch(start, [1] * 70, 8, 4, 64, 16))
+    check(ctx, Batch([3000, 20, 900], [1, 1, 1], 40, 2, 128, 16))
+    check(ctx, Batch([6000, 20, 900], [1, 2, 1], 6, 1, 256, 24))
+
+
 def test_offsets_beyond_32_bits(ctx):
     """A cache of more than 2^32 elements, its last pages in use."""
     pages, page, hkv, d = 2**32 // (1024 * 128) + 40, 64, 16, 128
