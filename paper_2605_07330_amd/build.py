@@ -11,7 +11,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libsrs.so")
 SOURCES = [os.path.join(HERE, "csrc", "srs.hip")]
-HEADERS = [os.path.join(HERE, "csrc", f) for f in ("srs_kernels.hpp", "cache_kernels.hpp", "attention_kernels.hpp", "device_guard.hpp", "scratch_array.hpp")] + [os.path.join(ROOT, "include", "srs.h")]
+HEADERS = [os.path.join(HERE, "csrc", f) for f in ("srs_kernels.hpp", "cache_kernels.hpp", "attention_kernels.hpp", "cache_calls.hpp", "device_guard.hpp", "scratch_array.hpp")] + [os.path.join(ROOT, "include", "srs.h")]
 
 
 def hipcc_command(out: str = LIB, extra=()) -> list:
