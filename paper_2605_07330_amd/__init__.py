@@ -1,4 +1,4 @@
-"""MI355X-native hot path of lossless sparse weight synchronisation (extract / apply).
+"""MI355X-native hot path of lossless sparse weight synchronisation (extract / apply), and the Rollout's key/value cache behind it.
 
 ``paper_2605_07330_amd.srs``   -- ctypes binding of the C-ABI library ``libsrs.so`` (HIP, gfx950).
 ``paper_2605_07330_amd.synth`` -- seeded synthetic workloads (inputs only).

@@ -235,8 +235,9 @@ __device__ __forceinline__ uint32_t parts_of(const AttnShape &w, int32_t all) {
 // read, K so that memory is read by whole rows, past the caches (128 requests of up to 8192 keys: 464 us with K straight from
 // memory in the operand's layout, half a line to an instruction, where the hint did nothing; 417 this way).  Pieces of 16 bytes are rearranged
 // in each row so that neither read meets itself on a bank.  The next tile's rows are in flight meanwhile.
-// Bound: the cache's bytes.  Weights meet the values in two parts (value and remainder of its rounding): the second product costs
-// nothing here.
+// Weights meet the values in two parts, value and remainder of its rounding, as the second product costs nothing here: the output is
+// then off by its own rounding alone.
+// Bound: the cache's bytes.  2.42 GB of them in 405 us (5.98 TB/s; two plain read streams reach 6.98), 0.60 GB of two requests in 104.
 template <class T, int DP, bool BLOCKS, bool EXACT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, DP == 64 ? 3 : DP == 128 ? 2 : 1) void attention_narrow_kernel(const AttnArgs a) {
     constexpr int kNarrowKeys = 32 * WAVES;
@@ -255,8 +256,7 @@ __global__ __launch_bounds__(64 * WAVES, DP == 64 ? 3 : DP == 128 ? 2 : 1) void 
     if (blockIdx.x == 0) check_requests(a);
     AttnTile t;
     if (!open_request(a, id / w.splits, t) || (uint32_t)t.n > a.narrow_most) return;
-    // one tile, unless the caller's hint was wrong
-    for (int32_t i0 = 0; i0 < t.n; i0 += (int32_t)w.tile_tokens) {
+    for (int32_t i0 = 0; i0 < t.n; i0 += (int32_t)w.tile_tokens) {                  // one tile, unless the caller's hint was wrong
     if (i0) __syncthreads();
     open_tile(a, i0, w.tile_tokens, t);
     const KeyTiles tiles(t, kNarrowKeys);
@@ -480,13 +480,17 @@ __global__ __launch_bounds__(64 * WAVES, DP == 64 ? 3 : DP == 128 ? 2 : 1) void 
 }
 
 // ---- many rows: chunks ---------------------------------------------------------------------------------------------------------
-// 128 rows to a workgroup, 32 to each of its four waves, which all go through the tile's keys, 64 at a time.  K and V of a key tile pass
-// through LDS (two buffers; the next tile is on its way in registers meanwhile), where every wave takes them as the left operand of
-// v_mfma 32x32x16: S^T = K Q^T, so that a lane holds the weights of one row, and O^T = V^T P^T with P^T straight from those registers, the
-// keys of a product counted in the order in which the lanes have them.  Pieces of 16 bytes are rearranged in each row so that neither
-// the rows of K nor the transposed reads of V meet on a bank.  Weights are rounded to the element type for the second product.  A row's
-// accumulators follow its running maximum only when that has grown by 2^kSlack.
-// Bound: the matrix units, then LDS reads and the exponentials beside them.
+// 128 rows to a workgroup, 32 to each of its four waves, which all go through the tile's keys, 64 at a time (32 above heads of 128).  K and
+// V of a key tile pass through LDS (two buffers; the next tile is on its way in registers meanwhile), where every wave takes them as
+// the left operand of v_mfma 32x32x16: S^T = K Q^T, so that a lane holds the weights of one row, and O^T = V^T P^T with P^T straight from
+// those registers, the keys of a product counted in the order in which the lanes have them.  Pieces of 16 bytes are rearranged in
+// each row so that neither the rows of K nor the transposed reads of V meet on a bank (no conflicts counted).  Weights are rounded to
+// the element type for the second product: of the order of the output's own rounding.  A row's accumulators follow its running maximum
+// only when that has grown by 2^kSlack.  Workgroups of a key head follow each other in steps of the number of key heads, so that an XCD
+// keeps few of them in its L2.
+// Bound: the matrix units, with the exponentials beside them.  8192 new tokens of 32 heads of 128 over 4 key heads, 550 GFLOP: 620 to 670 us
+// (820 to 890 TFLOP/s; a plain 8192^3 product 1120); matrix units busy 40 % of the time, vector units 46 %, LDS 30 %.  One row's scores
+// held a key tile ahead, so that products stand beside exponentials, fewer vector instructions for the maximum and wave priorities changed nothing.
 constexpr float kSlack = 8.f;
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 __device__ __forceinline__ f32x16 mfma_32x32x16(AttnTypes<__bf16>::x8 a, AttnTypes<__bf16>::x8 b, f32x16 c) {
