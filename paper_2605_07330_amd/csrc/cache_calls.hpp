@@ -227,8 +227,10 @@ extern "C" {
 // New tokens, and pages of the free list, that a workgroup of the table calls is there for, of 256 and 64 at most.  512 / 2048 / 8192 tokens, us:
 // 4,200 5.7 / 6.1 / 6.7, 34,000 6.0 / 6.7 / 10.2, 136,000 7.9 / 7.2 / 11.3; 1024 / 8192 / 65,536 pages of the list: 16,400 pages taken and
 // released 14.4 / 16.9 / 32.6, 64,000 19.5 / 23.3 / 83.1.
+// Where one is enough and requests are few it has 256 threads instead of 1024, whose sums and barriers are what such a call consists of: tables and release
+// together, 1024 / 256, us: 1 request 8.2 / 5.6, 128 of one token 9.7 / 7.0, 256 10.0 / 7.4, 64 of up to 16 9.6 / 8.2, 200 of up to 5 10.0 / 9.0.
 constexpr uint64_t kTokensEach = 1024;
-constexpr uint32_t kPagesEach = 1024;
+constexpr uint32_t kPagesEach = 1024, kFewRequests = 256;
 
 int srs_cache_tables(srs_ctx *ctx, const int32_t *start, const int32_t *count, uint32_t nrequests, uint32_t page_tokens,
                      int32_t *held, int32_t *table, uint32_t table_width, const int32_t *free_pages, int32_t *free_count,
@@ -245,7 +247,8 @@ int srs_cache_tables(srs_ctx *ctx, const int32_t *start, const int32_t *count, u
     TablesArgs a{start, count, nrequests, page_tokens, held, table, table_width, free_pages, free_count, free_cap,
                  token_begin, slots, positions, (uint32_t)max_tokens, ctx->flags, ctx->flags + kTicketWord};
     const uint64_t grid = (max_tokens + kTokensEach - 1) / kTokensEach;
-    hipLaunchKernelGGL(cache_tables_kernel, dim3((uint32_t)(grid < 1 ? 1 : grid > 256 ? 256 : grid)), dim3(kTableThreads), 0, st, a);
+    if (nrequests <= kFewRequests && grid <= 1) hipLaunchKernelGGL((cache_tables_kernel<256>), dim3(1), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((cache_tables_kernel<1024>), dim3((uint32_t)(grid < 1 ? 1 : grid > 256 ? 256 : grid)), dim3(1024), 0, st, a);
     SRS_HIP(hipGetLastError());
     return SRS_OK;
 }
@@ -260,7 +263,8 @@ int srs_cache_release(srs_ctx *ctx, const int32_t *keep, uint32_t nrequests, int
     SRS_ON_DEVICE(ctx->device);
     ReleaseArgs a{keep, nrequests, held, table, table_width, free_pages, free_count, free_cap, ctx->flags, ctx->flags + kTicketWord};
     const uint32_t grid = free_cap / kPagesEach;         // as if all that the list has room for came back
-    hipLaunchKernelGGL(cache_release_kernel, dim3(grid < 1 ? 1 : grid > 64 ? 64 : grid), dim3(kTableThreads), 0, st, a);
+    if (nrequests <= kFewRequests && grid <= 1) hipLaunchKernelGGL((cache_release_kernel<256>), dim3(1), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((cache_release_kernel<1024>), dim3(grid < 1 ? 1 : grid > 64 ? 64 : grid), dim3(1024), 0, st, a);
     SRS_HIP(hipGetLastError());
     return SRS_OK;
 }

@@ -6,7 +6,6 @@ namespace srs {
 
 // ---- block tables -----------------------------------------------------------------------------------------------------
 
-constexpr int kTableThreads = 1024;
 
 struct TablesArgs {
     const int32_t *start, *count;
@@ -35,6 +34,7 @@ __device__ __forceinline__ bool last_workgroup(uint32_t *ticket) {
 }
 
 // Exclusive sums of two numbers per thread over the workgroup; totals in the last two.
+template <int kTableThreads>
 __device__ __forceinline__ void block_sums(int64_t a, int64_t b, int64_t &before_a, int64_t &before_b, int64_t &all_a, int64_t &all_b) {
     __shared__ int64_t wave_sums[2][kTableThreads / 64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -71,6 +71,7 @@ __device__ __forceinline__ uint32_t last_at_most(const uint32_t *at, uint32_t n,
 // The pages that tokens lie in are known from the sums, whether they are in the table yet or not; the numbers that the call
 // changes are written by the workgroup that finishes last, when nobody reads them any more.  Bound: latency (a load, two sums, a
 // bisection, a load); from some 100,000 tokens on the slots' bytes.  One workgroup for everything took 485 us for 557,000 tokens of 256 requests.
+template <int kTableThreads>
 __global__ __launch_bounds__(kTableThreads) void cache_tables_kernel(const TablesArgs a) {
     __shared__ uint32_t s_tok[kTableThreads + 1], s_page[kTableThreads + 1], s_start[kTableThreads], s_held[kTableThreads];
     const uint32_t tid = threadIdx.x, worker = blockIdx.x * kTableThreads + tid, workers = gridDim.x * kTableThreads;
@@ -94,7 +95,7 @@ __global__ __launch_bounds__(kTableThreads) void cache_tables_kernel(const Table
             want = most > held ? (int64_t)(most - held) : 0;
         }
         int64_t t0, p0, t_all, p_all;
-        block_sums(cnt, want, t0, p0, t_all, p_all);
+        block_sums<kTableThreads>(cnt, want, t0, p0, t_all, p_all);
         t0 += tokens; p0 += pages;
         tokens += t_all; pages += p_all;
         s_tok[tid] = t0 < (int64_t)a.max_tokens ? (uint32_t)t0 : a.max_tokens;
@@ -162,6 +163,7 @@ struct ReleaseArgs {
 
 // The surplus pages, numbered in the order in which srs_cache_tables would have handed them out, go to the end of the free list from the
 // last to the first.
+template <int kTableThreads>
 __global__ __launch_bounds__(kTableThreads) void cache_release_kernel(const ReleaseArgs a) {
     __shared__ uint32_t s_page[kTableThreads + 1], s_keep[kTableThreads];
     const uint32_t tid = threadIdx.x, worker = blockIdx.x * kTableThreads + tid, workers = gridDim.x * kTableThreads;
@@ -183,14 +185,14 @@ __global__ __launch_bounds__(kTableThreads) void cache_release_kernel(const Rele
     int64_t all = 0, before = 0, x, y, n, z;
     for (uint32_t base = 0; base < a.nrequests; base += kTableThreads) {       // how many there are
         look(base);
-        block_sums(extra, 0, x, y, n, z);
+        block_sums<kTableThreads>(extra, 0, x, y, n, z);
         all += n;
     }
     for (uint32_t base = 0; base < a.nrequests; base += kTableThreads) {
         const uint32_t count = a.nrequests - base < (uint32_t)kTableThreads ? a.nrequests - base : (uint32_t)kTableThreads;
         if (a.nrequests > (uint32_t)kTableThreads) {                            // else they are still there
             look(base);
-            block_sums(extra, 0, x, y, n, z);
+            block_sums<kTableThreads>(extra, 0, x, y, n, z);
         }
         s_page[tid] = (uint32_t)x; s_keep[tid] = keep;
         if (tid == count - 1) s_page[count] = (uint32_t)n;
