@@ -32,6 +32,8 @@ struct AttnArgs {
     uint32_t narrow_most;                                           // requests of more new tokens are the wide kernel's
     uint32_t split_tokens;                                          // of more: not split by the narrow kernel
     uint32_t wide_tiles;                                            // 0: there is no wide launch
+    bool ranked;                                                    // up to kRanked requests, in order of length
+    uint32_t places;                                                // wide workgroups that the card holds, where the last round's are shared out; else 0
 };
 
 template <class T> struct AttnTypes;
@@ -227,6 +229,62 @@ __device__ __forceinline__ uint32_t parts_of(const AttnShape &w, int32_t all) {
     const uint32_t n = ((uint32_t)all + w.split_tiles - 1) / w.split_tiles;
     return n < 1 ? 1 : n > w.splits ? w.splits : n;
 }
+
+// Up to 64 requests, one to a lane, whose tiles are taken from the one with the longest keys on, later tokens first, so that the last
+// workgroups are short ones.  In the batch's order / in this and the last round shared out as below, us: 24 requests of up to 512 new tokens
+// behind up to 4096, heads of 64, 276 / 266, 60 of up to 64 behind 4000 143 / 112; heads of 128, 16 of up to 300 behind 8000 308 / 286.
+constexpr uint32_t kRanked = 64;
+struct Ranked {
+    int32_t first_row, n, start;
+    uint32_t tiles, before, all;        // this lane's, those of the requests before it, and all
+    __device__ __forceinline__ Ranked(const AttnArgs &a, uint32_t tile_tokens) {
+        const uint32_t lane = threadIdx.x & 63;
+        AttnTile t;
+        const bool open = lane < a.nrequests && open_request(a, lane, t) && (uint32_t)t.n > a.narrow_most;
+        first_row = open ? t.first_row : 0; n = open ? t.n : 0; start = open ? (int32_t)t.start : 0;
+        tiles = ((uint32_t)n + tile_tokens - 1) / tile_tokens;
+        const uint32_t place = (((uint32_t)start + (uint32_t)n) & ~63u) | (63u - lane);      // the longest in steps of 64 keys, then the first
+        before = all = 0;
+        for (uint32_t r = 0; r < a.nrequests; r += 4) {
+#pragma unroll
+            for (uint32_t k = 0; k < 4; ++k) {
+                const uint32_t its = (uint32_t)__builtin_amdgcn_readlane((int)tiles, (int)(r + k)), its_place = (uint32_t)__builtin_amdgcn_readlane((int)place, (int)(r + k));
+                before += its_place > place ? its : 0u;
+                all += its;
+            }
+        }
+    }
+    // Request and first token of tile `at` of all; -1 where there are fewer.
+    __device__ __forceinline__ int32_t find(uint32_t at, uint32_t tile_tokens, AttnTile &t) const {
+        const uint64_t here = __ballot(at - before < tiles);
+        if (!here) return -1;
+        const int r = __builtin_ctzll(here);
+        t.r = r;
+        t.first_row = __builtin_amdgcn_readlane(first_row, r); t.n = __builtin_amdgcn_readlane(n, r); t.start = __builtin_amdgcn_readlane(start, r);
+        const uint32_t its = (uint32_t)__builtin_amdgcn_readlane((int)tiles, r), its_before = (uint32_t)__builtin_amdgcn_readlane((int)before, r);
+        return (int32_t)((its - 1 - (at - its_before)) * tile_tokens);
+    }
+};
+
+// Workgroups beyond the last whole number of rounds on a card of `places` leave most of it idle while they run: from `full` on, each of
+// `units` is shared out over `most` workgroups, whose results go to part_o [places][128][head_dim] and part_lse [places][128].
+// One request, whole workgroups on 512 places / the last round shared out, us: 552 of them over 30,000 keys 1785 / 1220, over 8000
+// 497 / 368, over 1500 129 / 117; 1056 over 8000 832 / 713, 1552 1210 / 1085, 2600 2090 / 1965.
+constexpr uint32_t kTailParts = 16, kTailTiles = 4;     // at most, and key tiles of a part at least
+struct Tail {
+    uint32_t units, full, most;
+    __device__ __forceinline__ Tail(uint32_t n, uint32_t places) {
+        const uint32_t rest = places && n > places ? n % places : 0u;
+        most = rest ? places / rest : 1u;
+        most = most < kTailParts ? most : kTailParts;
+        units = n; full = most > 1 ? n - rest : n;
+    }
+    __device__ __forceinline__ uint32_t each(int32_t all) const {
+        const uint32_t e = ((uint32_t)all + most - 1) / most;
+        return e < kTailTiles ? kTailTiles : e;
+    }
+    __device__ __forceinline__ uint32_t parts(int32_t all) const { return all > 0 ? ((uint32_t)all + each(all) - 1) / each(all) : 1u; }
+};
 
 // ---- few rows: decoding ------------------------------------------------------------------------------------------------------
 // 16 rows to a workgroup, 32 keys of a tile to each of its four or eight waves, which join their results at the end.  Scores come as
@@ -511,21 +569,42 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_wide_kernel(
     __shared__ int32_t s_dirty;                                                    // was a value not finite
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform_value(tid >> 6), h = lane >> 5, n = lane & 31;
     const AttnShape &w = a.wide;
-    uint32_t id = blockIdx.x;
-    const uint32_t hb = id % (a.kv_heads * w.head_blocks), kh = hb / w.head_blocks, block = hb % w.head_blocks;
-    id /= a.kv_heads * w.head_blocks;
-    const uint32_t split = id % w.splits, tile = a.wide_tiles - 1 - id / w.splits;  // later tokens, which see more keys, first
+    const uint32_t heads = a.kv_heads * w.head_blocks;
+    uint32_t unit = blockIdx.x / (heads * w.splits) * heads + blockIdx.x % heads, split = blockIdx.x / heads % w.splits, tail_part = 0;
     AttnTile t;
-    const int32_t r = find_request(a, tile, w.tile_tokens, 1);
-    if (r < 0 || !open_request(a, (uint32_t)r, t) || (uint32_t)t.n <= a.narrow_most) return;
-    const int64_t i0 = (int64_t)(tile - ((uint32_t)t.first_row / w.tile_tokens + (uint32_t)r)) * w.tile_tokens;
-    if (i0 >= t.n) return;
-    open_tile(a, (int32_t)i0, w.tile_tokens, t);
+    Tail tail(0, 0);
+    if (a.ranked) {
+        const Ranked order(a, w.tile_tokens);
+        tail = Tail(order.all * heads, a.places);
+        if (tail.most > 1 && blockIdx.x >= tail.full) {                             // w.splits is 1 then
+            tail_part = blockIdx.x - tail.full;
+            if (tail_part / tail.most >= tail.units - tail.full) return;
+            unit = tail.full + tail_part / tail.most; split = tail_part % tail.most;
+        }
+        const int32_t i0 = order.find(unit / heads, w.tile_tokens, t);
+        if (i0 < 0) return;
+        open_tile(a, i0, w.tile_tokens, t);
+    } else {
+        const uint32_t tile = a.wide_tiles - 1 - unit / heads;                      // later tokens, which see more keys, first
+        const int32_t r = find_request(a, tile, w.tile_tokens, 1);
+        if (r < 0 || !open_request(a, (uint32_t)r, t) || (uint32_t)t.n <= a.narrow_most) return;
+        const int64_t i0 = (int64_t)(tile - ((uint32_t)t.first_row / w.tile_tokens + (uint32_t)r)) * w.tile_tokens;
+        if (i0 >= t.n) return;
+        open_tile(a, (int32_t)i0, w.tile_tokens, t);
+    }
+    // the same in all lanes, which the compiler does not see behind the two ways
+    t.r = uniform_value(t.r); t.first_row = uniform_value(t.first_row); t.n = uniform_value(t.n); t.i0 = uniform_value(t.i0); t.i1 = uniform_value(t.i1);
+    t.end = uniform_value(t.end); t.low = uniform_value(t.low); t.sinks = uniform_value(t.sinks); t.start = uniform_value((int32_t)t.start);
+    unit = uniform_value(unit); split = uniform_value(split);
+    const uint32_t hb = unit % heads, kh = hb / w.head_blocks, block = hb % w.head_blocks;
     const KeyTiles tiles(t, KT);
-    const uint32_t parts = parts_of(w, tiles.all);
+    const bool in_tail = tail.most > 1 && unit >= tail.full;
+    const uint32_t parts = in_tail ? tail.parts(tiles.all) : parts_of(w, tiles.all), each_part = in_tail ? tail.each(tiles.all) : w.split_tiles;
     if (split >= parts) return;
-    const int32_t from = (int32_t)(split * w.split_tiles);
-    int32_t to = split + 1 == parts ? tiles.all : from + (int32_t)w.split_tiles;
+    // one part: ~0, one of the last round's: its number, top bit set, else the part's: as one number, it costs the loop one register
+    const uint32_t part = uniform_value(parts == 1 ? ~0u : in_tail ? tail_part | 1u << 31 : split);
+    const int32_t from = (int32_t)(split * each_part);
+    int32_t to = split + 1 == parts ? tiles.all : from + (int32_t)each_part;
     if (a.pages == 0) to = from;
     bool bad = t.narrow || (a.pages == 0 && tiles.all > 0);
 
@@ -729,7 +808,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_wide_kernel(
     const bool some = !(m == -INFINITY && l == 0.f);
     const float inv = some ? 1.f / l : 0.f;
     const uint32_t out_head = kh * a.group + head;
-    const uint64_t cell = (split * w.slots + row) * a.heads + out_head;                         // where parts > 1
+    const uint64_t cell = part >> 31 ? (uint64_t)(part & 0x7fffffffu) * 128 + slot : (part * w.slots + row) * a.heads + out_head;
     auto each = [&](auto store) {
 #pragma unroll
         for (int d = 0; d < kDB; ++d)
@@ -740,7 +819,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_wide_kernel(
                     store(at, some ? o[d][4 * u] * inv : 0.f, some ? o[d][4 * u + 1] * inv : 0.f, some ? o[d][4 * u + 2] * inv : 0.f, some ? o[d][4 * u + 3] * inv : 0.f);
             }
     };
-    if (parts > 1) {
+    if (part != ~0u) {
         float *const to_p = w.part_o + cell * a.head_dim;
         each([&](uint32_t at, float y0, float y1, float y2, float y3) { *(f32x4 *)(to_p + at) = f32x4{y0, y1, y2, y3}; });
     } else {
@@ -749,7 +828,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_wide_kernel(
     }
     if (h == 0) {
         const float lse2 = some ? m + __builtin_amdgcn_logf(l) - kShift : -INFINITY;
-        if (parts > 1) w.part_lse[cell] = lse2;
+        if (part != ~0u) w.part_lse[cell] = lse2;
         else if (a.lse) a.lse[row * a.heads + out_head] = lse2 * 0.69314718055994530942f;
     }
 }
@@ -762,11 +841,60 @@ constexpr int kSplitKeys = 128;                             // keys of a tile of
 // (171 parts: 17 us with 8 groups, 11 with 32).
 constexpr uint32_t kFewParts = 8;
 
+struct Joined {
+    float L;
+    f32x4 x;                            // lane: elements 4 * lane on
+};
+// Parts `from`, from + step and so on, to each half of the wave its own.
+__device__ __forceinline__ Joined join_parts(const AttnArgs &a, const float *lse, const float *part, uint64_t stride, uint32_t from, uint32_t step, uint32_t n, float base) {
+    const uint32_t lane = threadIdx.x & 63, piece = lane & 31;
+    float L = 0.f;
+    f32x4 o[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll 4
+    for (uint32_t s = from; s < n; s += step) {
+        const float share = __builtin_amdgcn_exp2f(lse[s * stride] - base);
+        L += share;
+        const float *p = part + s * stride * a.head_dim;
+        if (piece * 4 < a.head_dim) o[0] += share * *(const f32x4 *)(p + piece * 4);
+        if (piece * 4 + 128 < a.head_dim) o[1] += share * *(const f32x4 *)(p + piece * 4 + 128);
+    }
+    L += __shfl_xor(L, 32);
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[k][e] += __shfl_xor(o[k][e], 32);
+    return Joined{L, lane < 32 ? o[0] : o[1]};
+}
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+    for (int k = 1; k < 64; k *= 2) x = fmaxf(x, __shfl_xor(x, k));
+    return x;
+}
+template <class T>
+__device__ __forceinline__ void store_joined(const AttnArgs &a, const Joined &y, float M, float base, uint64_t row, uint32_t head) {
+    typedef typename AttnTypes<T>::x4 x4;
+    const uint32_t lane = threadIdx.x & 63;
+    const bool some = !(M == -INFINITY && y.L == 0.f);
+    if (lane * 4 < a.head_dim) {
+        const float inv = some ? 1.f / y.L : 0.f;
+        *(x4 *)((T *)a.out + (int64_t)row * a.o_token + (int64_t)head * a.o_head + lane * 4) =
+            x4{(T)(some ? y.x[0] * inv : 0.f), (T)(some ? y.x[1] * inv : 0.f), (T)(some ? y.x[2] * inv : 0.f), (T)(some ? y.x[3] * inv : 0.f)};
+    }
+    if (lane == 0 && a.lse) a.lse[row * a.heads + head] = some ? (base + __builtin_amdgcn_logf(y.L)) * 0.69314718055994530942f : -INFINITY;
+}
+// A wave joins n parts that lie `stride` cells apart.
+template <class T>
+__device__ __forceinline__ void join_row(const AttnArgs &a, const float *lse, const float *part, uint64_t stride, uint32_t n, uint64_t row, uint32_t head) {
+    const uint32_t lane = threadIdx.x & 63;
+    float M = -INFINITY;
+    for (uint32_t s = lane; s < n; s += 64) M = fmaxf(M, lse[s * stride]);
+    M = wave_max(M);
+    const float base = M == -INFINITY ? 0.f : M;
+    store_joined<T>(a, join_parts(a, lse, part, stride, lane >> 5, 2, n, base), M, base, row, head);
+}
+
 template <class T, bool WIDE, bool MANY>
 __global__ __launch_bounds__(MANY ? 1024 : 256) void attention_join_kernel(const AttnArgs a) {
-    constexpr int kWaves = MANY ? 16 : 1;
-    __shared__ float s_top[kWaves], s_sum[kWaves];
-    __shared__ f32x4 s_o[kWaves][MANY ? 64 : 1];
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform_value(tid >> 6);
     const AttnShape &w = WIDE ? a.wide : a.narrow;
     const uint64_t cell = MANY ? blockIdx.x : (uint64_t)blockIdx.x * 4 + wave;
@@ -789,52 +917,54 @@ __global__ __launch_bounds__(MANY ? 1024 : 256) void attention_join_kernel(const
     if (n <= 1) return;
     const uint64_t row = (uint64_t)t.first_row + i, stride = w.slots * a.heads;
     const float *const lse = w.part_lse + cell, *const part = w.part_o + cell * a.head_dim;
-    float M = -INFINITY;
-    for (uint32_t s = MANY ? tid : lane; s < n; s += 64 * kWaves) M = fmaxf(M, lse[s * stride]);
-#pragma unroll
-    for (int x = 1; x < 64; x *= 2) M = fmaxf(M, __shfl_xor(M, x));
-    if constexpr (MANY) {
+    if constexpr (!MANY) {
+        join_row<T>(a, lse, part, stride, n, row, head);
+    } else {
+        constexpr int kWaves = 16;
+        __shared__ float s_top[kWaves], s_sum[kWaves];
+        __shared__ f32x4 s_o[kWaves][64];
+        float M = -INFINITY;
+        for (uint32_t s = tid; s < n; s += 64 * kWaves) M = fmaxf(M, lse[s * stride]);
+        M = wave_max(M);
         if (lane == 0) s_top[wave] = M;
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < kWaves; ++k) M = fmaxf(M, s_top[k]);
-    }
-    const float base = M == -INFINITY ? 0.f : M;
-    const uint32_t group = (MANY ? tid : lane) >> 5, piece = lane & 31;
-    float L = 0.f;
-    f32x4 o[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-#pragma unroll 4
-    for (uint32_t s = group; s < n; s += 2 * kWaves) {
-        const float share = __builtin_amdgcn_exp2f(lse[s * stride] - base);
-        L += share;
-        const float *p = part + s * stride * a.head_dim;
-        if (piece * 4 < a.head_dim) o[0] += share * *(const f32x4 *)(p + piece * 4);
-        if (piece * 4 + 128 < a.head_dim) o[1] += share * *(const f32x4 *)(p + piece * 4 + 128);
-    }
-    L += __shfl_xor(L, 32);
-#pragma unroll
-    for (int k = 0; k < 2; ++k)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[k][e] += __shfl_xor(o[k][e], 32);
-    f32x4 x = lane < 32 ? o[0] : o[1];                                              // lane: elements 4 * lane on
-    if constexpr (MANY) {
-        s_o[wave][lane] = x;
-        if (lane == 0) s_sum[wave] = L;
+        const float base = M == -INFINITY ? 0.f : M;
+        Joined y = join_parts(a, lse, part, stride, tid >> 5, 2 * kWaves, n, base);
+        s_o[wave][lane] = y.x;
+        if (lane == 0) s_sum[wave] = y.L;
         __syncthreads();
         if (wave) return;
-        L = 0.f;
-        x = f32x4{0.f, 0.f, 0.f, 0.f};
+        y.L = 0.f;
+        y.x = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int k = 0; k < kWaves; ++k) { L += s_sum[k]; x += s_o[k][lane]; }
+        for (int k = 0; k < kWaves; ++k) { y.L += s_sum[k]; y.x += s_o[k][lane]; }
+        store_joined<T>(a, y, M, base, row, head);
     }
-    const bool some = !(M == -INFINITY && L == 0.f);
-    if (lane * 4 < a.head_dim) {
-        const float inv = some ? 1.f / L : 0.f;
-        typedef typename AttnTypes<T>::x4 x4;
-        *(x4 *)((T *)a.out + (int64_t)row * a.o_token + (int64_t)head * a.o_head + lane * 4) =
-            x4{(T)(some ? x[0] * inv : 0.f), (T)(some ? x[1] * inv : 0.f), (T)(some ? x[2] * inv : 0.f), (T)(some ? x[3] * inv : 0.f)};
+}
+
+// The parts of the last round's workgroups, row by row (11,000 rows in 8 parts of heads of 64 14 us, none 4; on twice and four times the workgroups
+// the same within the scatter).
+template <class T>
+__global__ __launch_bounds__(256) void attention_tail_join_kernel(const AttnArgs a) {
+    const AttnShape &w = a.wide;
+    const uint32_t wave = uniform_value(threadIdx.x >> 6), heads = a.kv_heads * w.head_blocks;
+    const Ranked order(a, w.tile_tokens);
+    const Tail tail(order.all * heads, a.places);
+    if (tail.most <= 1) return;
+    for (uint32_t at = blockIdx.x * 4 + wave; at < (tail.units - tail.full) * 128; at += gridDim.x * 4) {
+        const uint32_t first_part = at / 128 * tail.most, slot = at % 128, unit = tail.full + at / 128, hb = unit % heads;
+        AttnTile t;
+        const int32_t i0 = order.find(unit / heads, w.tile_tokens, t);
+        if (i0 < 0) return;
+        open_tile(a, i0, w.tile_tokens, t);
+        const uint32_t n = tail.parts(KeyTiles(t, a.head_dim <= 128 ? 64 : 32).all);
+        const uint32_t token = slot / w.block, head = hb % w.head_blocks * w.block + slot % w.block;
+        if (n <= 1 || t.i0 + (int32_t)token >= t.i1 || head >= a.group || token >= w.tile_tokens) continue;
+        const uint64_t cell = (uint64_t)first_part * 128 + slot;
+        join_row<T>(a, w.part_lse + cell, w.part_o + cell * a.head_dim, 128, n, (uint64_t)(t.first_row + i0) + token, hb / w.head_blocks * a.group + head);
     }
-    if (lane == 0 && a.lse) a.lse[row * a.heads + head] = some ? (base + __builtin_amdgcn_logf(L)) * 0.69314718055994530942f : -INFINITY;
 }
 
 }  // namespace srs

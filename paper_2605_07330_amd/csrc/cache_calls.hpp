@@ -84,6 +84,8 @@ constexpr uint64_t kMaxKeys = 1ull << 30;              // of one request
 struct AttnPlan {
     AttnShape narrow, wide;
     uint32_t narrow_most, split_tokens, wide_tiles;
+    uint32_t places;                    // of the wide kernel's workgroups, where its last round is shared out; else 0
+    bool ranked;                        // requests in order of length
     bool eight;                         // waves of the narrow kernel, instead of four
     uint64_t workspace;
 };
@@ -95,9 +97,11 @@ struct AttnPlan {
 // over 30,000 140 / 130 / 143, 512 over 8000 136 / 113 / 122; four of 64 over 16,000 187 / 134 / 189).  At least 2 / 4 / 8 key tiles: 16 rows
 // over 8000 keys 27 / 25 / 29.
 // Where tiles nearly fill the card without parts (three quarters of those workgroups), parts cost the wide kernel a pass over all results:
-// 528 full tiles of 35 key tiles 152 us, in two parts 178.  Tiles of few rows come in two all the same, which evens out the end: 64 requests
+// 528 full tiles of 35 key tiles 152 us, in two parts 178.  Those behind the last whole round are shared out instead (116), where there are at
+// most kTailRounds of them, which bounds the gain, and kTailKeys key tiles, which pay for the join.  Tiles of few rows come in two all the same, which evens out the end: 64 requests
 // of 5 rows over 4000 keys 276 / 226.
 constexpr uint64_t kNarrowWorkgroups = 12 * 256, kWideWorkgroups = 512;
+constexpr uint64_t kTailKeys = 24, kTailRounds = 6;
 constexpr uint64_t kLeastNarrowTiles = 2, kLeastWideTiles = 4, kFewRows = 32;
 
 // The narrow kernel's parts are joined by a launch of their own.  The workgroup that ends last could do it, but what the others wrote has to
@@ -150,7 +154,7 @@ AttnPlan attention_plan(uint32_t nrequests, uint64_t tokens, uint32_t q_heads, u
     p.narrow_most = only_narrow ? 0x7fffffffu : p.narrow.tile_tokens;
     p.split_tokens = only_narrow ? (uint32_t)most_tokens : p.narrow.tile_tokens;
     p.narrow.slots = (uint64_t)nrequests * p.split_tokens;
-    p.wide.slots = tokens; p.wide.splits = 1; p.wide.split_tiles = 0x7fffffff; p.wide_tiles = 0;
+    p.wide.slots = tokens; p.wide.splits = 1; p.wide.split_tiles = 0x7fffffff; p.wide_tiles = 0; p.places = 0; p.ranked = false;
     if (!only_narrow) {
         p.wide_tiles = (uint32_t)(tokens / p.wide.tile_tokens + nrequests);
         // of the tiles, those that hold something: a request's last is the only one that may be less than full
@@ -159,17 +163,19 @@ AttnPlan attention_plan(uint32_t nrequests, uint64_t tokens, uint32_t q_heads, u
         const bool nearly_full = wide_units * 4 >= kWideWorkgroups * 3, few_rows = tokens * group <= kFewRows * wide_busy;
         attention_split(p.wide, wide_keys, !nearly_full ? parts_over(wide_units * wide_keys, kWideWorkgroups)
                                           : few_rows && wide_units < 2 * kWideWorkgroups ? parts_over(wide_keys, 2) : wide_keys, kLeastWideTiles);
+        const uint32_t places = 256 * (head_dim <= 64 ? 3 : head_dim <= 128 ? 2 : 1);                  // registers allow so many
+        p.ranked = nrequests <= kRanked && p.wide.splits == 1 && wide_units > places;
+        if (p.ranked && wide_keys >= kTailKeys && wide_units <= kTailRounds * places) p.places = places;
     }
     p.workspace = 0;
     if (p.narrow.splits > 1) p.workspace += p.narrow.splits * p.narrow.slots * q_heads * 4 * (head_dim + 4);
     if (p.wide.splits > 1) p.workspace += p.wide.splits * p.wide.slots * q_heads * 4 * (head_dim + 4);
+    p.workspace += (uint64_t)p.places * 128 * 4 * (head_dim + 4);
     return p;
 }
 
 // Where the parts lie in the workspace: results, then their lse (four words' room for each, which keeps what follows aligned).
-void attention_parts(AttnShape &w, uint32_t q_heads, uint32_t head_dim, float *&at) {
-    if (w.splits <= 1) return;
-    const uint64_t cells = w.splits * w.slots * q_heads;
+void attention_parts(AttnShape &w, uint64_t cells, uint32_t head_dim, float *&at) {
     w.part_o = at; w.part_lse = at + cells * head_dim;
     at += cells * (head_dim + 4);
 }
@@ -192,7 +198,7 @@ int launch_join(const AttnArgs &a, const AttnShape &w, hipStream_t st) {
 
 template <class T, int DP>
 int launch_attention(const AttnArgs &a, bool blocks, bool eight, hipStream_t st) {
-    const dim3 narrow(a.nrequests * a.narrow.splits * a.kv_heads * a.narrow.head_blocks), wide(a.wide_tiles * a.wide.splits * a.kv_heads * a.wide.head_blocks);
+    const dim3 narrow(a.nrequests * a.narrow.splits * a.kv_heads * a.narrow.head_blocks), wide(a.wide_tiles * a.wide.splits * a.kv_heads * a.wide.head_blocks + a.places);
 #define SRS_ATTENTION(BLOCKS, EXACT)                                                                                    \
     do {                                                                                                                \
         if (a.wide_tiles) {                                                                                             \
@@ -211,6 +217,10 @@ int launch_attention(const AttnArgs &a, bool blocks, bool eight, hipStream_t st)
 #undef SRS_ATTENTION
     int rc = launch_join<T, false>(a, a.narrow, st);
     if (rc == SRS_OK) rc = launch_join<T, true>(a, a.wide, st);
+    if (rc == SRS_OK && a.places) {
+        hipLaunchKernelGGL((attention_tail_join_kernel<T>), dim3(1024), dim3(256), 0, st, a);
+        SRS_HIP(hipGetLastError());
+    }
     return rc;
 }
 
@@ -341,7 +351,7 @@ int srs_cache_attention(srs_ctx *ctx, const srs_cache *cache, const srs_rows *q,
                                       most_tokens, most_keys);
     if (p.workspace && (!workspace || ((uintptr_t)workspace & 15u) || workspace_bytes < p.workspace)) return SRS_ERR_INVALID;
     if (!grid_ok((uint64_t)nrequests * p.narrow.splits * cache->heads * p.narrow.head_blocks, p.eight ? 512 : 256) ||
-        !grid_ok((uint64_t)p.wide_tiles * p.wide.splits * cache->heads * p.wide.head_blocks, 256) || tokens * q->heads > 0x7fffffffull ||
+        !grid_ok((uint64_t)p.wide_tiles * p.wide.splits * cache->heads * p.wide.head_blocks + p.places, 256) || tokens * q->heads > 0x7fffffffull ||
         (p.narrow.splits > 1 && !grid_ok(p.narrow.slots * q->heads, p.narrow.splits <= kFewParts ? 64 : 1024)) ||
         (p.wide.splits > 1 && !grid_ok(p.wide.slots * q->heads, p.wide.splits <= kFewParts ? 64 : 1024)))
         return SRS_ERR_INVALID;
@@ -363,10 +373,11 @@ int srs_cache_attention(srs_ctx *ctx, const srs_cache *cache, const srs_rows *q,
     a.window = window; a.sinks = sinks; a.full = (flags & SRS_ATTN_FULL) != 0; a.flags = ctx->flags;
     a.scale = scale == 0.f ? 1.f : std::fabs(scale) * 1.44269504088896340736f;
     a.sign = scale > 0.f ? 1.f : scale < 0.f ? -1.f : 0.f;
-    a.narrow = p.narrow; a.wide = p.wide; a.narrow_most = p.narrow_most; a.split_tokens = p.split_tokens; a.wide_tiles = p.wide_tiles;
+    a.narrow = p.narrow; a.wide = p.wide; a.narrow_most = p.narrow_most; a.split_tokens = p.split_tokens; a.wide_tiles = p.wide_tiles; a.ranked = p.ranked; a.places = p.places;
     float *at = (float *)workspace;
-    attention_parts(a.narrow, q->heads, cache->head_dim, at);
-    attention_parts(a.wide, q->heads, cache->head_dim, at);
+    if (p.narrow.splits > 1) attention_parts(a.narrow, p.narrow.splits * p.narrow.slots * q->heads, cache->head_dim, at);
+    if (p.wide.splits > 1) attention_parts(a.wide, p.wide.splits * p.wide.slots * q->heads, cache->head_dim, at);
+    if (p.places) attention_parts(a.wide, (uint64_t)p.places * 128, cache->head_dim, at);
     const bool blocks = in_blocks(cache);
     if (cache->dtype == SRS_BF16) return launch_attention<__bf16>(a, blocks, p.eight, st);
     return launch_attention<_Float16>(a, blocks, p.eight, st);

@@ -386,6 +386,74 @@ def test_parts_of_many_requests(ctx):
     check(ctx, Batch([6000, 20, 900], [1, 2, 1], 6, 1, 256, 24))
 
 
+# Workgroups a little over one or two rounds of the card: heads wide, head dimension, start and count of the requests, page.
+ROUNDS = [(64, 64, 128, [1000], [1029], 16), (64, 64, 64, [200], [1539], 16), (32, 32, 256, [100], [2049], 16), (128, 16, 128, [1500], [521], 64),
+          (192, 48, 72, [0, 3000, 700, 5], [200, 90, 1, 60], 24), (48, 48, 96, [1100, 1100, 2000], [128, 1300, 1], 16)]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("hq,hkv,d,start,count,page", ROUNDS)
+def test_a_last_round_of_few_workgroups(ctx, dtype, hq, hkv, d, start, count, page):
+    """What is left after whole rounds is shared out and joined; rows behind the last sequence stay."""
+    batch = Batch(start, count, hq, hkv, d, page, dtype, extra_rows=40)
+    want = batch.expect()
+    T = sum(count)
+    want = tuple(x[:T] for x in want)
+    out, lse = batch.call(ctx, most_tokens=max(count), most_keys=max(s + c for s, c in zip(start, count)))
+    compare((out, lse), want)
+    assert bool((out[T:] == 9.0).all() and (lse[T:] == 9.0).all()) and ctx.status() == 0
+    again = batch.call(ctx, out=batch.q)                                        # the queries' own place, without hints
+    compare(again, want)
+
+
+@pytest.mark.parametrize("kw", [{"window": 1500, "sinks": 40}, {"causal": False}, {"scale": -0.3}])
+def test_a_last_round_otherwise(ctx, kw):
+    batch = Batch([2500], [521], 128, 16, 128, 16)
+    check(ctx, batch, **kw)
+
+
+def test_a_last_round_with_holes_and_junk(ctx):
+    """Its keys miss a page; values that only some rows see are not finite."""
+    from paper_2605_07330_amd import srs
+    batch = Batch([1500], [521], 128, 16, 128, 16)
+    first, last = batch.table[0, 1503 // 16].item(), batch.table[0, 2020 // 16].item()
+    batch.v[first, 1503 % 16, 2, 7] = math.inf
+    batch.v[last, 2020 % 16, 3] = math.nan
+    batch.table[0, 40] = -1
+    check(ctx, batch, flags=srs.FLAG_BAD_INDEX)
+
+
+def test_sixty_four_requests_of_all_lengths(ctx):
+    """As many as are put in order by the length of their keys; equal lengths and empty requests among them."""
+    start = [(r * 37) % 300 if r % 5 else 128 for r in range(64)]
+    count = [(0, 1, 3, 40, 70, 129)[r % 6] for r in range(64)]
+    check(ctx, Batch(start, count, 8, 2, 64, 16))
+    check(ctx, Batch(start + [9], count + [33], 8, 2, 64, 16))                  # one more
+
+
+def test_a_last_round_from_a_graph(ctx):
+    from paper_2605_07330_amd import srs
+    batch = Batch([1500], [521], 128, 16, 128, 16)
+    want = batch.expect()
+    out, lse = torch.full_like(batch.q, 9.0), torch.full(batch.q.shape[:2], 9.0, device=DEV)
+    need = srs.attention_workspace(1, 521, 128, 16, 128, batch.table.shape[1], 16, most_tokens=521, most_keys=2021)
+    assert need
+    room = torch.empty(need, dtype=torch.uint8, device=DEV)
+    call = lambda: batch.call(ctx, out=out, lse=lse, most_tokens=521, most_keys=2021, workspace=room)
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for _ in range(3):
+        out.fill_(9.0)
+        lse.fill_(9.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        compare((out, lse), want)
+    assert ctx.status() == 0
+
+
 def test_offsets_beyond_32_bits(ctx):
     """A cache of more than 2^32 elements, its last pages in use."""
     pages, page, hkv, d = 2**32 // (1024 * 128) + 40, 64, 16, 128
