@@ -441,8 +441,9 @@ int srs_cache_write(srs_ctx *ctx, const srs_cache *cache, const srs_rows *k, con
  * sinks need a window).  A row that sees no key is 0, its lse -inf.  Hidden keys and values do not enter, whatever their bits are.  Rows
  * outside every request are left as they are.  out may be q with the same strides, and otherwise overlaps nothing.
  * Sums, maxima and products are binary32, and out is rounded once.  Where a request has few new tokens (those of 16 / (q->heads /
- * cache->heads), at least one) the weights exp(s_j) meet the values in two parts of the element type, otherwise rounded to it; weights
- * below 2^-126 of a row's largest are 0.  The same call gives the same bits each time.
+ * cache->heads), at least one) the weights exp(s_j) meet the values in two parts of the element type, otherwise rounded to it, as closely
+ * for small weights as for large ones; those below 2^-126 of a row's largest are 0, and FP16 adds up to 2^-75 of the largest to each one's
+ * error.  The same call gives the same bits each time.
  * q, out and cache are BF16 or FP16; head_dim a multiple of 8 up to 256; q->heads a multiple of cache->heads; every pointer 16-byte
  * aligned and every stride a multiple of 8 elements.  lse (tokens x q->heads, contiguous) may be NULL.  A page outside the cache that a
  * row would read counts as hidden and raises SRS_FLAG_BAD_INDEX, as does a request whose rows lie outside 0 .. tokens (it is left out).  Keys

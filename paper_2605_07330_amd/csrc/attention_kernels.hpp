@@ -46,7 +46,7 @@ template <> struct AttnTypes<__bf16> {
 template <> struct AttnTypes<_Float16> {
     typedef _Float16 x8 __attribute__((ext_vector_type(8)));
     typedef _Float16 x4 __attribute__((ext_vector_type(4)));
-    // weights are carried times 2^12: halves lose bits below 2^-14, where the weights of a long row of keys lie
+    // weights are carried times 2^12, as halves lose bits below 2^-14; what they still lose goes in products of its own (kLift)
     static constexpr float kShift = 12.f;
     static constexpr uint32_t kExponent = 0x7c00u;
 };
@@ -79,6 +79,14 @@ template <class T> __device__ __forceinline__ u32x4 finite_values(u32x4 x) {
     for (int e = 0; e < 4; ++e) y[e] = x[e] & ((x[e] & E) == E ? 0xffff0000u : ~0u) & ((x[e] >> 16 & E) == E ? 0xffffu : ~0u);
     return y;
 }
+
+// Halves hold numbers to within 2^-25.  What they lose so of a weight below 2^-14 (or, in two halves, below 2^-3) is added times 2^40 by products of
+// its own in those tiles that have such weights; what these lose again is 2^-65, which not even 2^30 keys of the largest value make a half of.
+// Without it a key whose value is 0 and whose score lies 20 above 8000 others took 10 % of the result, 24 above all of it.  us, lost / added: scores of
+// unit spread, 8192 re-encoded, heads of 128, 694 / 717, 24 chunks of heads of 64 261 / 277, a decoding batch 414 / 416; of spread 4, where
+// nearly every tile has such weights, 705 / 1142, 270 / 436 and 415 / 423.
+constexpr float kLift = 0x1p40f;
+__device__ __forceinline__ float lost_weight(float x, float left, float below) { return fabsf(x) < below ? left * kLift : 0.f; }
 
 // Queries take the scale's sign, so that the largest score is that of the largest product; 0 where there is none.
 template <class T> __device__ __forceinline__ typename AttnTypes<T>::x8 signed_query(typename AttnTypes<T>::x8 q, bool there, float sign) {
@@ -299,6 +307,7 @@ struct Tail {
 template <class T, int DP, bool BLOCKS, bool EXACT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, DP == 64 ? 3 : DP == 128 ? 2 : 1) void attention_narrow_kernel(const AttnArgs a) {
     constexpr int kNarrowKeys = 32 * WAVES;
+    constexpr bool kHalf = AttnTypes<T>::kShift != 0.f;
     typedef typename AttnTypes<T>::x8 x8;
     typedef typename AttnTypes<T>::x4 x4;
     constexpr int kQC = DP / 32, kVC = DP / 16, kRegion = 64 * DP + 256, kRowPieces = DP / 8;      // 32 rows of V, or 16 of float results; pieces of 16 bytes
@@ -432,7 +441,7 @@ __global__ __launch_bounds__(64 * WAVES, DP == 64 ? 3 : DP == 128 ? 2 : 1) void 
         const uint32_t here = (uint32_t)ok;
         if (more) load(next);
         next = ask(tiles.key(i + 2, kNarrowKeys) + shift, i + 2 < to);
-        float x[8], top = -INFINITY;
+        float x[8], top = -INFINITY, low = INFINITY;
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             f32x4 s = {0.f, 0.f, 0.f, 0.f};
@@ -440,6 +449,10 @@ __global__ __launch_bounds__(64 * WAVES, DP == 64 ? 3 : DP == 128 ? 2 : 1) void 
             for (int c = 0; c < kQC; ++c) s = mfma_16x16x32(*(const x8 *)(keys + k_place(16 * b + n, 4 * c + g)), q[c], s);
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[4 * b + e] = s[e] * a.scale;
+        }
+        if constexpr (kHalf) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) low = fminf(low, x[e]);
         }
         if (!whole) {
             const uint32_t sees = ((uint32_t)seen_bits(key, row_low, row_end, t.sinks) & here) >> (4 * g);
@@ -472,6 +485,21 @@ __global__ __launch_bounds__(64 * WAVES, DP == 64 ? 3 : DP == 128 ? 2 : 1) void 
             const x8 vt = __builtin_bit_cast(x8, __builtin_shufflevector(values(c, 0), values(c, 1), 0, 1, 2, 3, 4, 5, 6, 7));
             o[c] = mfma_16x16x32(vt, high, o[c]);
             o[c] = mfma_16x16x32(vt, rest, o[c]);
+        }
+        if constexpr (kHalf) {
+            if (__any(low - base < -3.f)) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    x[e] = lost_weight(x[e], x[e] - (float)high[e] - (float)rest[e], 0x1p-3f);
+                    high[e] = (T)x[e];
+                    rest[e] = (T)(x[e] - (float)high[e]);
+                }
+#pragma unroll
+                for (int c = 0; c < kVC; ++c) {
+                    const x8 vt = __builtin_bit_cast(x8, __builtin_shufflevector(values(c, 0), values(c, 1), 0, 1, 2, 3, 4, 5, 6, 7));
+                    o[c] += mfma_16x16x32(vt, rest, mfma_16x16x32(vt, high, f32x4{0.f, 0.f, 0.f, 0.f})) * (1.f / kLift);
+                }
+            }
         }
     }
     if (dirty) {
@@ -544,12 +572,11 @@ __global__ __launch_bounds__(64 * WAVES, DP == 64 ? 3 : DP == 128 ? 2 : 1) void 
 // those registers, the keys of a product counted in the order in which the lanes have them.  Pieces of 16 bytes are rearranged in
 // each row so that neither the rows of K nor the transposed reads of V meet on a bank (no conflicts counted).  Weights are rounded to
 // the element type for the second product: of the order of the output's own rounding.  A row's accumulators follow its running maximum
-// only when that has grown by 2^kSlack.  Workgroups of a key head follow each other in steps of the number of key heads, so that an XCD
+// only when that has grown by 2^kSlack (less in halves, where it costs the small weights bits).  Workgroups of a key head follow each other in steps of the number of key heads, so that an XCD
 // keeps few of them in its L2.
 // Bound: the matrix units, with the exponentials beside them.  8192 new tokens of 32 heads of 128 over 4 key heads, 550 GFLOP: 620 to 670 us
 // (820 to 890 TFLOP/s; a plain 8192^3 product 1120); matrix units busy 40 % of the time, vector units 46 %, LDS 30 %.  One row's scores
 // held a key tile ahead, so that products stand beside exponentials, fewer vector instructions for the maximum and wave priorities changed nothing.
-constexpr float kSlack = 8.f;
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 __device__ __forceinline__ f32x16 mfma_32x32x16(AttnTypes<__bf16>::x8 a, AttnTypes<__bf16>::x8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
@@ -559,12 +586,13 @@ __device__ __forceinline__ f32x16 mfma_32x32x16(AttnTypes<_Float16>::x8 a, AttnT
 }
 
 template <class T, int DP, bool BLOCKS, bool EXACT>
-__global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_wide_kernel(const AttnArgs a) {
+__global__ __launch_bounds__(256, DP == 64 ? 3 : DP == 128 ? 2 : 1) void attention_wide_kernel(const AttnArgs a) {
     typedef typename AttnTypes<T>::x8 x8;
     typedef typename AttnTypes<T>::x4 x4;
     constexpr int KT = DP <= 128 ? 64 : 32, kB = KT / 32, kQC = DP / 16, kDB = DP / 32, kRowPieces = DP / 8;
     constexpr int kRowsPerLoad = 256 / kRowPieces, kRowsPerWave = kRowsPerLoad / 4, kLoads = KT / kRowsPerLoad, kBytes = KT * DP * 2;
-    constexpr float kShift = AttnTypes<T>::kShift == 0.f ? 0.f : 6.f;              // with kSlack: at most 2^14 in a half
+    constexpr bool kHalf = AttnTypes<T>::kShift != 0.f;
+    constexpr float kSlack = kHalf ? 4.f : 8.f, kShift = kHalf ? 10.f : 0.f;         // at most 2^14 in a half
     __shared__ __attribute__((aligned(16))) unsigned char s_k[2][kBytes], s_v[2][kBytes];
     __shared__ int32_t s_dirty;                                                    // was a value not finite
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform_value(tid >> 6), h = lane >> 5, n = lane & 31;
@@ -730,7 +758,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_wide_kernel(
         next = ask(tiles.key(i + 2, KT), i + 2 < to);
         if (key < any_end && (key + KT > any_low || key < t.sinks)) {              // some row of the wave sees something
             const bool whole = key + KT <= all_end && (key >= all_low || key + KT <= t.sinks) && !holes;
-            float x[kB][16], top = -INFINITY;
+            float x[kB][16], top = -INFINITY, low = INFINITY;
 #pragma unroll
             for (int b = 0; b < kB; ++b) {
                 f32x16 s;
@@ -740,6 +768,10 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_wide_kernel(
                 for (int c = 0; c < kQC; ++c) s = mfma_32x32x16(*(const x8 *)(s_k[buf] + k_place(32 * b + n, 2 * c + h)), q[c], s);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) x[b][e] = s[e];
+                if constexpr (kHalf) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) low = fminf(low, s[e]);
+                }
             }
             if (!whole) {
                 uint64_t sees = seen_bits(key, row_low, row_end, t.sinks);
@@ -763,6 +795,36 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_wide_kernel(
                 m = m2;
             }
             const float base = kShift - (m == -INFINITY ? 0.f : m);
+            if constexpr (kHalf) {
+                if (__any(__builtin_fmaf(low, a.scale, base) < -14.f)) {
+                    // copies that the compiler cannot see through: it would keep what it has here, registers full of it, for the products below
+                    float base_here = base;
+                    uint32_t key_here = 0;
+                    asm volatile("" : "+v"(base_here), "+v"(key_here));
+                    auto values_here = [&](int d, int b, int c, int u) {
+                        return lds_transposed(s_v[buf] + v_place(key_here + 32 * b + 16 * c + 8 * u + 4 * h + ((lane & 15) >> 2), 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + (lane & 1) * 8);
+                    };
+#pragma unroll
+                    for (int d = 0; d < kDB; ++d) o[d] *= kLift;
+#pragma unroll
+                    for (int b = 0; b < kB; ++b)
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            x8 r;
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][8 * c + e], a.scale, base_here));
+                                r[e] = (T)lost_weight(y, y - (float)(T)y, 0x1p-14f);
+                            }
+#pragma unroll
+                            for (int d = 0; d < kDB; ++d)
+                                o[d] = mfma_32x32x16(__builtin_bit_cast(x8, __builtin_shufflevector(values_here(d, b, c, 0), values_here(d, b, c, 1), 0, 1, 2, 3, 4, 5, 6, 7)), r, o[d]);
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+#pragma unroll
+                    for (int d = 0; d < kDB; ++d) o[d] *= 1.f / kLift;
+                }
+            }
             x8 p[kB][2];
 #pragma unroll
             for (int b = 0; b < kB; ++b)
