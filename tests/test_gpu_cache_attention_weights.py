@@ -97,3 +97,34 @@ def test_weights_of_every_size(ctx, dtype, hq, hkv, d, page, start, count):  # n
     grow = (60000.0 * torch.exp(-score - 30.0)).clamp(max=60000.0)[..., None]
     b.v[:] = (grow * torch.rand(b.v.shape, generator=g, device=DEV)).to(dtype)
     compare(ctx, b, 1.0)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("hq,hkv,d,start", [(8, 2, 128, [3, 20, 50]), (32, 8, 128, [40]), (4, 4, 64, [7, 60]), (16, 1, 256, [33, 12]), (6, 2, 80, [30])])
+def test_few_tokens_have_weights_in_two_parts(ctx, dtype, hq, hkv, d, start):  # noqa: F811
+    """Values come in pairs of opposite sign behind keys that are nearly alike, so that the result is small beside what it is the sum of and its own
+    rounding hides nothing: weights rounded once would be seen, which the oracle with such weights shows first."""
+    b = Batch(start, [1] * len(start), hq, hkv, d, 16, dtype, seed=d)
+    g = torch.Generator(device=DEV).manual_seed(d)
+    b.q.zero_()
+    b.q[..., 2] = 1.0
+    b.k.zero_()
+    b.k[..., 2] = (-2.0 * torch.rand(b.k.shape[:3], generator=g, device=DEV)).to(dtype)
+    for r in range(len(start)):
+        page, place = dense(b, r)
+        n = page.numel() // 2 * 2
+        b.k[page[1:n:2], place[1:n:2], :, 2] = 1.03125 * b.k[page[0:n:2], place[0:n:2], :, 2]
+        b.v[page[1:n:2], place[1:n:2]] = -b.v[page[0:n:2], place[0:n:2]]
+        if page.numel() % 2:
+            b.v[page[-1], place[-1]] = 0.0
+    for r in range(len(start)):
+        want, tol = exact(b, r, 1.0, True)
+        page, place = dense(b, r)
+        seen = False
+        for head in range(hq):
+            s = b.q[r:r + 1, head].double() @ b.k[page, place, head // (hq // hkv)].double().t().contiguous()
+            p = (s - s.amax()).exp()
+            once = p.to(dtype).double() @ b.v[page, place, head // (hq // hkv)].double() / p.sum()
+            seen |= bool(((once - want[:, head]).abs() > tol[:, head]).any())
+        assert seen, "the data would not show weights that are rounded once"
+    compare(ctx, b, 1.0)
