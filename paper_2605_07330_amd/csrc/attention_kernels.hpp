@@ -88,6 +88,17 @@ template <class T> __device__ __forceinline__ u32x4 finite_values(u32x4 x) {
 constexpr float kLift = 0x1p40f;
 __device__ __forceinline__ float lost_weight(float x, float left, float below) { return fabsf(x) < below ? left * kLift : 0.f; }
 
+// A part of a result under its share of the weights.  A value that is not finite is itself, also where the part lies so far below the others that
+// its share is 0.
+__device__ __forceinline__ void add_part(f32x4 &sum, float share, f32x4 part) {
+    if (share != 0.f) {
+        sum += share * part;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] += fabsf(part[e]) < INFINITY ? 0.f : part[e];
+    }
+}
+
 // Queries take the scale's sign, so that the largest score is that of the largest product; 0 where there is none.
 template <class T> __device__ __forceinline__ typename AttnTypes<T>::x8 signed_query(typename AttnTypes<T>::x8 q, bool there, float sign) {
     typename AttnTypes<T>::x8 y;
@@ -542,12 +553,10 @@ __global__ __launch_bounds__(64 * WAVES, DP == 64 ? 3 : DP == 128 ? 2 : 1) void 
     for (int c = 0; c < DP / 64; ++c) {
         const uint32_t d = c * 64 + (tid & 15) * 4;
         if (d >= a.head_dim) continue;
-        float y[4] = {0.f, 0.f, 0.f, 0.f};
+        f32x4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < WAVES; ++k) {
-            const f32x4 part = *(const f32x4 *)((const float *)(s_mem + k * kRegion) + orow * (DP + 4) + d);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] += share[k] * part[e];
+            add_part(y, share[k], *(const f32x4 *)((const float *)(s_mem + k * kRegion) + orow * (DP + 4) + d));
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) y[e] = some ? y[e] * inv : 0.f;
@@ -917,8 +926,8 @@ __device__ __forceinline__ Joined join_parts(const AttnArgs &a, const float *lse
         const float share = __builtin_amdgcn_exp2f(lse[s * stride] - base);
         L += share;
         const float *p = part + s * stride * a.head_dim;
-        if (piece * 4 < a.head_dim) o[0] += share * *(const f32x4 *)(p + piece * 4);
-        if (piece * 4 + 128 < a.head_dim) o[1] += share * *(const f32x4 *)(p + piece * 4 + 128);
+        if (piece * 4 < a.head_dim) add_part(o[0], share, *(const f32x4 *)(p + piece * 4));
+        if (piece * 4 + 128 < a.head_dim) add_part(o[1], share, *(const f32x4 *)(p + piece * 4 + 128));
     }
     L += __shfl_xor(L, 32);
 #pragma unroll
