@@ -209,6 +209,17 @@ def _not_negative(where: str, *sizes: int) -> None:
         raise SrsError(ERR_INVALID, where)
 
 
+def _fit_32_bits(where: str, *sizes: int) -> None:
+    """ctypes would drop the bits above: the library could not refuse what it does not see.  Its own limits lie below 2^31."""
+    if min(sizes) < 0 or max(sizes) > 0x7fffffff:
+        raise SrsError(ERR_INVALID, where)
+
+
+def _hints_ok(where: str, *hints: int) -> None:
+    if min(hints) < 0 or max(hints) >= 1 << 64:
+        raise SrsError(ERR_INVALID, where)
+
+
 def _payload_ok(I: torch.Tensor, V: torch.Tensor, counts: torch.Tensor, nb: int, cap: int, width: int = 2) -> None:
     if not (I.is_cuda and I.dtype == torch.int32 and I.is_contiguous() and I.numel() >= nb * cap):
         raise TypeError("I: expected contiguous int32 GPU tensor of at least nb*cap elements")
@@ -689,7 +700,7 @@ class Context:
             raise TypeError(f"table: expected [{n}, width]")
         if positions.numel() < slots.numel():
             raise ValueError("positions is shorter than slots")
-        _not_negative("srs_cache_tables", page_tokens)
+        _fit_32_bits("srs_cache_tables", page_tokens, n, table.shape[1], free_pages.numel())
         _check(_lib.srs_cache_tables(self._h, self._here(start, "start", i32), self._here(count, "count", i32, n), n, page_tokens,
                                      self._here(held, "held", i32, n), self._here(table, "table", i32), table.shape[1],
                                      self._here(free_pages, "free_pages", i32), self._here(free_count, "free_count", i32, 1),
@@ -706,6 +717,7 @@ class Context:
         i32, n = torch.int32, keep.numel()
         if table.dim() != 2 or table.shape[0] != n:
             raise TypeError(f"table: expected [{n}, width]")
+        _fit_32_bits("srs_cache_release", n, table.shape[1], free_pages.numel())
         _check(_lib.srs_cache_release(self._h, self._here(keep, "keep", i32), n, self._here(held, "held", i32, n),
                                       self._here(table, "table", i32), table.shape[1], self._here(free_pages, "free_pages", i32),
                                       self._here(free_count, "free_count", i32, 1), free_pages.numel(), st), "srs_cache_release")
@@ -722,6 +734,7 @@ class Context:
         if out.shape != x.shape:
             raise ValueError("x and out differ in shape")
         rx, ro = self._rows(x, "x", T, d, x.dtype), self._rows(out, "out", T, d, x.dtype)
+        _fit_32_bits("srs_rope", heads, d, 2 * inv_freq.numel())
         _check(_lib.srs_rope(self._h, _DTYPES[x.dtype], C.byref(rx), C.byref(ro), T, d, self._here(positions, "positions", torch.int32, T),
                              self._here(inv_freq, "inv_freq", torch.float64), 2 * inv_freq.numel(), flags, magnitude, st),
                "srs_rope")
@@ -747,6 +760,8 @@ class Context:
             if not rot or q_out is None:
                 raise TypeError("q: needs q_out, positions and inv_freq")
             rq, ro = C.byref(self._rows(q, "q", T, d, dt)), C.byref(self._rows(q_out, "q_out", T, d, dt))
+            _fit_32_bits("srs_cache_write", q.shape[1], q_out.shape[1])
+        _fit_32_bits("srs_cache_write", *k_cache.shape, k.shape[1], v.shape[1], rot)
         _check(_lib.srs_cache_write(self._h, C.byref(cache), C.byref(rk), C.byref(rv), T, self._here(slots, "slots", torch.int64), rq, ro, pos,
                                     freq, rot, flags, magnitude, st), "srs_cache_write")
 
@@ -766,7 +781,8 @@ class Context:
         rq, ro = self._rows(q, "q", T, d, k_cache.dtype), self._rows(out, "out", T, d, k_cache.dtype)
         if table.dim() != 2 or table.shape[0] != n:
             raise TypeError(f"table: expected [{n}, width]")
-        _not_negative("srs_cache_attention", window, sinks, most_tokens, most_keys)
+        _fit_32_bits("srs_cache_attention", window, sinks, n, table.shape[1], q.shape[1], out.shape[1], *k_cache.shape)
+        _hints_ok("srs_cache_attention", most_tokens, most_keys)
         need = _lib.srs_cache_attention_workspace(n, T, rq.heads, cache.heads, d, table.shape[1], cache.page_tokens, window, sinks,
                                                   most_tokens, most_keys)
         if need and workspace is None:
@@ -798,6 +814,8 @@ class Context:
 def attention_workspace(nrequests: int, tokens: int, q_heads: int, kv_heads: int, head_dim: int, table_width: int, page_tokens: int,
                         window: int = 0, sinks: int = 0, most_tokens: int = 0, most_keys: int = 0) -> int:
     """Bytes of workspace that cache_attention needs for these sizes."""
+    _fit_32_bits("srs_cache_attention_workspace", nrequests, tokens, q_heads, kv_heads, head_dim, table_width, page_tokens, window, sinks)
+    _hints_ok("srs_cache_attention_workspace", most_tokens, most_keys)
     return int(_lib.srs_cache_attention_workspace(nrequests, tokens, q_heads, kv_heads, head_dim, table_width, page_tokens, window, sinks,
                                                   most_tokens, most_keys))
 
