@@ -824,11 +824,17 @@ def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "none",
                      fast_turns: float = 32.0, slow_turns: float = 1.0, device=None) -> tuple:
     """(inv_freq, magnitude) for ``Context.rope`` and ``Context.cache_write``: angle per position of each of the rot_dim / 2 pairs, float64.
 
-    ``none``    base ** (-2 i / rot_dim)
-    ``linear``  the same over ``factor``: positions run ``factor`` times slower
-    ``base``    the base times factor ** (rot_dim / (rot_dim - 2)): the slowest pair runs ``factor`` times slower, the fastest as before
-    ``parts``   pairs that turn at least ``fast_turns`` times over ``original_context`` positions as before, those that turn at most
-                ``slow_turns`` times ``factor`` times slower, a linear mixture between; magnitude 0.1 log(factor) + 1
+    ``none``            base ** (-2 i / rot_dim)
+    ``linear``          the same over ``factor``: positions run ``factor`` times slower
+    ``base``            the base times factor ** (rot_dim / (rot_dim - 2)): the slowest pair runs ``factor`` times slower, the fastest as before
+    ``turns``           pairs that turn at least ``fast_turns`` times over ``original_context`` positions as before, those that turn at most
+                        ``slow_turns`` times ``factor`` times slower, between them a mixture that is linear in the turns
+    ``parts``           the same, with magnitude 0.1 log(factor) + 1
+    ``parts by index``  the same magnitude, the mixture linear in the pair's index i, from the last whole index at or before the one that turns
+                        ``fast_turns`` times to the first at or behind the one that turns ``slow_turns`` times
+
+    Keys match those of an engine only where it mixes the same way: a model whose configuration names such parts may be served with either
+    mixture (the frequencies between differ by up to some two times), so take the one that its weights were trained or are served with.
     """
     if rot_dim <= 0 or rot_dim % 2 or base <= 0 or factor < 1:
         raise ValueError("rot_dim: even and positive; base: positive; factor: at least 1")
@@ -838,13 +844,22 @@ def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "none",
     inv, magnitude = base ** (-i / rot_dim), 1.0
     if scaling == "linear":
         inv = inv / factor
-    elif scaling == "parts":
+    elif scaling in ("turns", "parts", "parts by index"):
         if original_context <= 0 or fast_turns <= slow_turns:
-            raise ValueError("parts: needs original_context, and fast_turns above slow_turns")
-        kept = ((inv * original_context / (2 * math.pi) - slow_turns) / (fast_turns - slow_turns)).clamp(0, 1)
-        inv, magnitude = inv * (kept + (1 - kept) / factor), 0.1 * math.log(factor) + 1.0
+            raise ValueError(f"{scaling}: needs original_context, and fast_turns above slow_turns")
+        if scaling == "parts by index":
+            if base <= 1 or slow_turns <= 0:
+                raise ValueError("parts by index: needs a base above 1, and slow_turns above 0")
+            first, last = (rot_dim / 2 * math.log(original_context / (2 * math.pi * turns)) / math.log(base) for turns in (fast_turns, slow_turns))
+            first, last = max(math.floor(first), 0), min(math.ceil(last), rot_dim - 1)
+            kept = ((last - i / 2) / max(last - first, 1e-3)).clamp(0, 1)
+        else:
+            kept = ((inv * original_context / (2 * math.pi) - slow_turns) / (fast_turns - slow_turns)).clamp(0, 1)
+        inv = inv * (kept + (1 - kept) / factor)
+        if scaling != "turns":
+            magnitude = 0.1 * math.log(factor) + 1.0
     elif scaling not in ("none", "base"):
-        raise ValueError(f"scaling {scaling!r}: none, linear, base or parts")
+        raise ValueError(f"scaling {scaling!r}: none, linear, base, turns, parts or parts by index")
     return inv.to(device), magnitude
 
 
