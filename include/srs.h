@@ -448,6 +448,9 @@ int srs_cache_write(srs_ctx *ctx, const srs_cache *cache, const srs_rows *k, con
  * aligned and every stride a multiple of 8 elements.  lse (tokens x q->heads, contiguous) may be NULL.  A page outside the cache that a
  * row would read counts as hidden and raises SRS_FLAG_BAD_INDEX, as does a request whose rows lie outside 0 .. tokens (it is left out).  Keys
  * beyond table_width pages are hidden and raise it too.
+ * scale times log2(e) has to be finite.  A row whose every score is -inf is taken as one that sees no key.  An infinite value that a row
+ * sees makes it infinite whatever its weight, two of opposite signs not a number.  Sums are taken before their division: BF16 values beyond
+ * 2^120 over the number of keys may come out infinite.
  * most_tokens and most_keys: the largest count and the largest number of keys of a request, as far as the caller knows (0: unknown).
  * They choose how the work is split, nothing else.
  * table_width * page_tokens is at most 2^30, tokens * q->heads below 2^31.

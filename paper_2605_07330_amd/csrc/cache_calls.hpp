@@ -79,6 +79,7 @@ int launch_rope(RopeArgs &a, int dtype, uint32_t flags, hipStream_t st) {
 
 namespace {
 constexpr uint64_t kMaxKeys = 1ull << 30;              // of one request
+constexpr float kLog2e = 1.44269504088896340736f;
 
 // How the attention of one call is laid out.
 struct AttnPlan {
@@ -337,7 +338,7 @@ int srs_cache_attention(srs_ctx *ctx, const srs_cache *cache, const srs_rows *q,
                         const int32_t *token_begin, const int32_t *start, const int32_t *table, uint32_t table_width,
                         uint32_t nrequests, float scale, uint32_t flags, uint32_t window, uint32_t sinks, uint64_t most_tokens,
                         uint64_t most_keys, void *workspace, uint64_t workspace_bytes, void *stream) {
-    if (!ctx || !cache || tokens > kMaxIndexable || nrequests > kMaxIndexable || (flags & ~SRS_ATTN_FULL) || !std::isfinite(scale)) return SRS_ERR_INVALID;
+    if (!ctx || !cache || tokens > kMaxIndexable || nrequests > kMaxIndexable || (flags & ~SRS_ATTN_FULL) || !std::isfinite(scale * kLog2e)) return SRS_ERR_INVALID;
     if ((cache->dtype != SRS_BF16 && cache->dtype != SRS_FP16) || !cache_ok(cache, 16)) return SRS_ERR_INVALID;
     if (cache->head_dim > 256 || (cache->head_dim & 7u) || window > kMaxIndexable || sinks > kMaxIndexable || (sinks && !window)) return SRS_ERR_INVALID;
     if ((flags & SRS_ATTN_FULL) && (window || sinks)) return SRS_ERR_INVALID;
@@ -371,7 +372,7 @@ int srs_cache_attention(srs_ctx *ctx, const srs_cache *cache, const srs_rows *q,
     a.page_magic = (uint32_t)(((1ull << (31 + log)) + cache->page_tokens - 1) / cache->page_tokens); a.page_shift = log ? log - 1 : 0;
     a.heads = q->heads; a.kv_heads = cache->heads; a.head_dim = cache->head_dim; a.group = q->heads / cache->heads;
     a.window = window; a.sinks = sinks; a.full = (flags & SRS_ATTN_FULL) != 0; a.flags = ctx->flags;
-    a.scale = scale == 0.f ? 1.f : std::fabs(scale) * 1.44269504088896340736f;
+    a.scale = scale == 0.f ? 1.f : std::fabs(scale) * kLog2e;
     a.sign = scale > 0.f ? 1.f : scale < 0.f ? -1.f : 0.f;
     a.narrow = p.narrow; a.wide = p.wide; a.narrow_most = p.narrow_most; a.split_tokens = p.split_tokens; a.wide_tiles = p.wide_tiles; a.ranked = p.ranked; a.places = p.places;
     float *at = (float *)workspace;
