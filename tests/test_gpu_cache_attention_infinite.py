@@ -60,3 +60,17 @@ def test_infinite_values_under_a_window(ctx, dtype, count):  # noqa: F811
     for key, element in ((1, 0), (1200, 1), (1930, 2), (1999, 3), (2000 + count - 1, 4)):
         put(b, 0, key, 1, element, math.inf)
     check(ctx, b, scale=1.0, window=700, sinks=3)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("start,count,hq,hkv,d,page", SHAPES[:-1])
+def test_scores_of_minus_infinity(ctx, dtype, start, count, hq, hkv, d, page):  # noqa: F811
+    """Keys with such scores weigh nothing; a row with no others is taken as one that sees no key."""
+    b = sloped(start, count, hq, hkv, d, page, dtype, 5, 2)
+    for r in range(len(start)):
+        page_of, place, _ = b.places(r)
+        b.k[page_of[::3], place[::3], :, 3] = -math.inf
+    check(ctx, b, scale=1.0)
+    b.k[..., 3] = -math.inf
+    out, lse = b.call(ctx, scale=1.0)
+    assert not bool(out.any()) and bool((lse == -math.inf).all()) and ctx.status() == 0
