@@ -84,11 +84,21 @@ template <class T> __device__ __forceinline__ u32x4 finite_values(u32x4 x) {
 
 // Halves hold numbers to within 2^-25.  What they lose so of a weight below 2^-14 (or, in two halves, below 2^-3) is added times 2^40 by products of
 // its own in those tiles that have such weights; what these lose again is 2^-65, which not even 2^30 keys of the largest value make a half of.
-// Without it a key whose value is 0 and whose score lies 20 above 8000 others took 10 % of the result, 24 above all of it.  us, lost / added: scores of
-// unit spread, 8192 re-encoded, heads of 128, 694 / 717, 24 chunks of heads of 64 261 / 277, a decoding batch 414 / 416; of spread 4, where
-// nearly every tile has such weights, 705 / 1142, 270 / 436 and 415 / 423.
+// Without it a key whose value is 0 and whose score lies 20 above 8000 others took 10 % of the result, 24 above all of it.  us, without this and without
+// looking at every value / as it is: scores of unit spread, 8192 re-encoded, heads of 128, 670 / 700, 24 chunks of heads of 64 261 / 268, 3000 tokens
+// over 1000, heads of 256, 490 / 529, a decoding batch 416 / 416; of spread 4, where nearly every tile has such weights, 673 / 1057, 258 / 412,
+// 514 / 1124 and 416 / 424.
 constexpr float kLift = 0x1p40f;
-__device__ __forceinline__ float lost_weight(float x, float left, float below) { return fabsf(x) < below ? left * kLift : 0.f; }
+// Of one half, and of two.  The bounds are held whole, so that larger weights taken as these lose nothing.
+__device__ __forceinline__ float lost_weight(float x) {
+    x = fminf(x, 0x1p-14f);
+    return (x - (float)(_Float16)x) * kLift;
+}
+__device__ __forceinline__ float lost_in_two(float x) {
+    x = fminf(x, 0x1p-3f);
+    const float rest = x - (float)(_Float16)x;
+    return (rest - (float)(_Float16)rest) * kLift;
+}
 
 // A part of a result under its share of the weights.  A value that is not finite is itself, also where the part lies so far below the others that
 // its share is 0.
@@ -503,7 +513,7 @@ __global__ __launch_bounds__(64 * WAVES, DP == 64 ? 3 : DP == 128 ? 2 : 1) void 
             if (__any(low - base < -3.f)) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    x[e] = lost_weight(x[e], x[e] - (float)high[e] - (float)rest[e], 0x1p-3f);
+                    x[e] = lost_in_two(x[e]);
                     high[e] = (T)x[e];
                     rest[e] = (T)(x[e] - (float)high[e]);
                 }
@@ -782,6 +792,8 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : DP == 128 ? 2 : 1) void attenti
                     for (int e = 0; e < 16; ++e) low = fminf(low, s[e]);
                 }
             }
+            // taken here, or the compiler keeps all scores beside what is left of them (277 / 271 us; above heads of 128 533 / 594)
+            if constexpr (kHalf && DP <= 128) asm volatile("" : "+v"(low));
             if (!whole) {
                 uint64_t sees = seen_bits(key, row_low, row_end, t.sinks);
                 if (holes) sees &= there_bits<BLOCKS, KT>(here);
@@ -823,7 +835,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : DP == 128 ? 2 : 1) void attenti
 #pragma unroll
                             for (int e = 0; e < 8; ++e) {
                                 const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][8 * c + e], a.scale, base_here));
-                                r[e] = (T)lost_weight(y, y - (float)(T)y, 0x1p-14f);
+                                r[e] = (T)lost_weight(y);
                             }
 #pragma unroll
                             for (int d = 0; d < kDB; ++d)
