@@ -326,7 +326,8 @@ struct Tail {
 // in each row so that neither read meets itself on a bank.  The next tile's rows are in flight meanwhile.
 // Weights meet the values in two parts, value and remainder of its rounding, as the second product costs nothing here: the output is
 // then off by its own rounding alone.
-// Bound: the cache's bytes.  2.42 GB of them in 405 us (5.98 TB/s; two plain read streams reach 6.98), 0.60 GB of two requests in 104.
+// Bound: the cache's bytes.  2.42 GB of them in 408 us (5.9 TB/s; two plain read streams reach 6.98), 0.60 GB of two requests in 106.  Heads of 256
+// leave one workgroup to a CU (132 KB of LDS): 8 requests of 8000 keys over 8 key heads 146 us, 3.6 TB/s.
 template <class T, int DP, bool BLOCKS, bool EXACT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, DP == 64 ? 3 : DP == 128 ? 2 : 1) void attention_narrow_kernel(const AttnArgs a) {
     constexpr int kNarrowKeys = 32 * WAVES;
@@ -593,11 +594,15 @@ __global__ __launch_bounds__(64 * WAVES, DP == 64 ? 3 : DP == 128 ? 2 : 1) void 
 // those registers, the keys of a product counted in the order in which the lanes have them.  Pieces of 16 bytes are rearranged in
 // each row so that neither the rows of K nor the transposed reads of V meet on a bank (no conflicts counted).  Weights are rounded to
 // the element type for the second product: of the order of the output's own rounding.  A row's accumulators follow its running maximum
-// only when that has grown by 2^kSlack (less in halves, where it costs the small weights bits).  Workgroups of a key head follow each other in steps of the number of key heads, so that an XCD
-// keeps few of them in its L2.
-// Bound: the matrix units, with the exponentials beside them.  8192 new tokens of 32 heads of 128 over 4 key heads, 550 GFLOP: 620 to 670 us
-// (820 to 890 TFLOP/s; a plain 8192^3 product 1120); matrix units busy 40 % of the time, vector units 46 %, LDS 30 %.  One row's scores
-// held a key tile ahead, so that products stand beside exponentials, fewer vector instructions for the maximum and wave priorities changed nothing.
+// only when that has grown by 2^kSlack (less in halves, where it costs the small weights bits).  Workgroups of a key head follow each other in
+// steps of the number of key heads, so that an XCD keeps few of them in its L2.
+// Bound: a wave's products and its exponentials, one after the other.  8192 new tokens of 32 heads of 128 over 4 key heads, 550 GFLOP: 640 to 680
+// us (810 to 860 TFLOP/s; a plain 8192^3 product 1120); matrix units busy 39 % of the time and vector units 50 %, which adds up to little less
+// than all of it: with 1.9 waves a SIMD they seldom work side by side.  One row's scores held a key tile ahead, so that products stand beside
+// exponentials, fewer vector instructions for the maximum and wave priorities changed nothing.
+// Of few rows: a wave owns 32 of the 128, so tiles of up to 32 rows keep one wave of four at the products, of up to 64 two: 16 tokens of
+// 32 heads over 8 key heads, 64 rows, take 27 us over 8000 keys and 72 over 60,000, whose bytes take 4.7 and 35.
+// Heads of 256: 256 + 256 registers and 128 bytes of scratch a lane, one wave a SIMD; 3000 tokens over 4000 at 530 TFLOP/s.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 __device__ __forceinline__ f32x16 mfma_32x32x16(AttnTypes<__bf16>::x8 a, AttnTypes<__bf16>::x8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);

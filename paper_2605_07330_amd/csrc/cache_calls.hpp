@@ -94,13 +94,13 @@ struct AttnPlan {
 // Workgroups that a launch should have where rows are few (two of either kernel fit a CU), and the fewest key tiles worth one.
 // The narrow kernel's are short and even out requests of unlike length; more are not worth their beginning and end (6 / 12 / 24 a CU,
 // us: 128 requests of up to 8192 keys 580 / 464 / 472, two of up to 131072 136 / 138 / 164).
-// The wide kernel's (256 / 512 / 1024, us, eight key heads, one request each: 16 rows over 60,000 keys 65 / 58 / 69, 32 118 / 77 / 74, 128
-// over 30,000 140 / 130 / 143, 512 over 8000 136 / 113 / 122; four of 64 over 16,000 187 / 134 / 189).  At least 2 / 4 / 8 key tiles: 16 rows
-// over 8000 keys 27 / 25 / 29.
+// The wide kernel's (256 / 512 / 1024, us, 32 heads over eight key heads, one request each: 16 tokens over 60,000 keys 65 / 58 / 69, 32
+// 118 / 77 / 74, 128 over 30,000 140 / 130 / 143, 512 over 8000 136 / 113 / 122; four of 64 over 16,000 187 / 134 / 189).  At least 2 / 4 / 8 key
+// tiles: 16 tokens over 8000 keys 27 / 25 / 29.
 // Where tiles nearly fill the card without parts (three quarters of those workgroups), parts cost the wide kernel a pass over all results:
 // 528 full tiles of 35 key tiles 152 us, in two parts 178.  Those behind the last whole round are shared out instead (116), where there are at
 // most kTailRounds of them, which bounds the gain, and kTailKeys key tiles, which pay for the join.  Tiles of few rows come in two all the same, which evens out the end: 64 requests
-// of 5 rows over 4000 keys 276 / 226.
+// of 5 tokens over 4000 keys 276 / 226.
 constexpr uint64_t kNarrowWorkgroups = 12 * 256, kWideWorkgroups = 512;
 constexpr uint64_t kTailKeys = 24, kTailRounds = 6;
 constexpr uint64_t kLeastNarrowTiles = 2, kLeastWideTiles = 4, kFewRows = 32;
