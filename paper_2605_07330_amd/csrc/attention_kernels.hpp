@@ -598,7 +598,7 @@ __global__ __launch_bounds__(64 * WAVES, DP == 64 ? 3 : DP == 128 ? 2 : 1) void 
 // steps of the number of key heads, so that an XCD keeps few of them in its L2.
 // Bound: a wave's products and its exponentials, one after the other.  8192 new tokens of 32 heads of 128 over 4 key heads, 550 GFLOP: 640 to 680
 // us (810 to 860 TFLOP/s; a plain 8192^3 product 1120); matrix units busy 39 % of the time and vector units 50 %, which adds up to little less
-// than all of it: with 1.9 waves a SIMD they seldom work side by side.  One row's scores held a key tile ahead, so that products stand beside
+// than all of it: with two waves a SIMD they seldom work side by side.  One row's scores held a key tile ahead, so that products stand beside
 // exponentials, fewer vector instructions for the maximum and wave priorities changed nothing.
 // Of few rows: a wave owns 32 of the 128, so tiles of up to 32 rows keep one wave of four at the products, of up to 64 two: 16 tokens of
 // 32 heads over 8 key heads, 64 rows, take 27 us over 8000 keys and 72 over 60,000, whose bytes take 4.7 and 35.
